@@ -302,6 +302,85 @@ xhc_status xhc_stream_expand(const xhc_handle* h, int64_t T, const uint16_t* hid
                              void* stream);
 xhc_status xhc_stream_sum(const xhc_handle* h, int64_t T, const uint16_t* X, uint16_t* y, void* stream);
 
+/* Types of gradient tensors (xhc_mlp_bwd, xhc_clip_grads). */
+typedef enum { XHC_F32 = 0, XHC_BF16 = 1 } xhc_dtype;
+
+/* The gated feed-forward block, the MLP sublayer F_t between pre_fwd(t) and post_fwd(t):
+ *   g = x gate^T, u = x up^T, h = act(g) * u, y = h down^T
+ * over T tokens, x and y [T, C] bf16; weights bf16, gate and up [F, C], down [C, F] (row-major: a row per
+ * output).  Products and the activation are formed in fp32; h, and in the backward the gradients of g and u
+ * (and the factors act(g) and u act'(g) that they are formed with), are rounded to bf16 as the operands of
+ * the next product.
+ *
+ * xhc_mlp_fwd writes y.  With `saved` (xhc_mlp_saved_bytes) it keeps there what the backward needs; null:
+ *   none is to come.
+ * xhc_mlp_bwd writes dx [T, C] bf16 and the weight gradients, shaped like the weights, in fp32
+ *   (XHC_F32; accumulate = 1 adds to what is there) or rounded once to bf16 (XHC_BF16; accumulate
+ *   has to be 0, else XHC_ERR_UNSUPPORTED).  x, W and `saved` are the forward's.
+ * `workspace` (xhc_mlp_workspace_bytes) is scratch of one call; a fresh one needs its first 256 bytes zeroed
+ * (its device error word, xhc_workspace_error).  Two calls in flight on different streams, or in two
+ * captured graphs that may run at once, need workspaces of their own.  x and y (dy and dx) may not overlap.
+ * Limits: C % 8 == 0, F % 8 == 0, 8 <= C <= 16384, 8 <= F <= 65536, 1 <= T <= 2^24, pointers 16-byte
+ * aligned; every result is the same, to the bit, from run to run. */
+typedef enum { XHC_ACT_SILU = 0, XHC_ACT_GELU = 1, XHC_ACT_RELU = 2 } xhc_act;   /* GELU: x Phi(x) */
+typedef struct {
+    int C;      /* hidden size                    */
+    int F;      /* width of the feed-forward block */
+    int act;    /* xhc_act                         */
+} xhc_mlp_config;
+typedef struct {
+    const uint16_t* gate;
+    const uint16_t* up;
+    const uint16_t* down;
+} xhc_mlp_weights;
+typedef struct {
+    void* gate;
+    void* up;
+    void* down;
+} xhc_mlp_grads;
+xhc_status xhc_mlp_saved_bytes(const xhc_mlp_config* cfg, int64_t T, size_t* bytes);
+xhc_status xhc_mlp_workspace_bytes(const xhc_mlp_config* cfg, int64_t T, size_t* bytes);
+xhc_status xhc_mlp_fwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weights* W, const uint16_t* x,
+                       uint16_t* y, void* saved, void* workspace, void* stream);
+xhc_status xhc_mlp_bwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weights* W, const uint16_t* x,
+                       const uint16_t* dy, uint16_t* dx, const xhc_mlp_grads* grads, int grad_dtype,
+                       int accumulate, const void* saved, void* workspace, void* stream);
+
+/* RMS norm of the sum of a token's N streams:
+ *   s = sum_i X[t][i], y[t] = w * s / sqrt(mean_c(s^2) + eps)
+ * X [T, N, C] bf16, w [C] fp32, y [T, C] bf16.  With the streams of a stack's last state it is the final
+ * reduction and norm in one pass (xhc_stream_sum rounds the sum to bf16 in between); with N = 1 it is the
+ * norm of a hidden vector, as a sublayer applies to its input.
+ * xhc_sum_norm_bwd writes dX [T, N, C] bf16 (the gradient of the sum, to every stream) and dw [C] fp32
+ * (accumulate = 1: adds to it; the tokens' terms are added in a fixed order).  `saved`
+ * (xhc_sum_norm_saved_bytes; null in the forward: no backward is to come) is the forward's; X is read
+ * again with N = 1 only and may be null otherwise.  `workspace` (xhc_sum_norm_workspace_bytes) is scratch
+ * of the backward.  Limits: 1 <= N <= 32, C % 8 == 0, 8 <= C <= 16384, eps >= 0, pointers 16-byte aligned. */
+xhc_status xhc_sum_norm_saved_bytes(int N, int C, int64_t T, size_t* bytes);
+xhc_status xhc_sum_norm_workspace_bytes(int N, int C, int64_t T, size_t* bytes);
+xhc_status xhc_sum_norm_fwd(int N, int C, float eps, int64_t T, const uint16_t* X, const float* w,
+                            uint16_t* y, void* saved, void* stream);
+xhc_status xhc_sum_norm_bwd(int N, int C, int64_t T, const uint16_t* X, const float* w, const uint16_t* dy,
+                            uint16_t* dX, float* dw, int accumulate, const void* saved, void* workspace,
+                            void* stream);
+
+/* The global norm of a training step's gradients, and their clipping:
+ *   norm = |scale| sqrt(sum over all tensors of g^2)
+ *   out  = g * scale * min(1, max_norm / (norm + eps))
+ * over n contiguous tensors, grads[q] of numel[q] values of type dtype[q] (xhc_dtype).  The library's
+ * gradients are sums over tokens, micro-batches and ranks: `scale` turns them into means in the same pass.
+ * out[q] receives tensor q and may be grads[q]; out null: all in place (nothing is written where the
+ * factor is 1).  Overlap other than that is not allowed.  The four arrays are host memory and are read
+ * before the call returns; tensors need no more than their own type's alignment (16 bytes is fastest).
+ * The squares are added in 64 bits where fp32 could lose one, and the sum always; the order is fixed.  `norm` (device, may be
+ * null) receives the norm; max_norm = infinity only measures and scales.  A norm that is not finite
+ * makes the factor what the formula says (0 for infinity, so that infinite gradients become NaN; NaN
+ * for NaN): check it before taking the step.
+ * `workspace`: xhc_clip_workspace_bytes, no initial content.  n <= 45000. */
+xhc_status xhc_clip_workspace_bytes(size_t* bytes);
+xhc_status xhc_clip_grads(int n, void* const* grads, void* const* out, const int64_t* numel, const int* dtype,
+                          double scale, double max_norm, double eps, float* norm, void* workspace, void* stream);
+
 /* Routing and pre-maps for callers that cannot allocate device memory.
  *
  * The paper has no counterpart: this is a deployment convenience.  Some callers cannot provide

@@ -1,9 +1,11 @@
 // libxhc C ABI: validation, buffer layout and the launch sequence of each entry point.
+#include <math.h>
 #include <stdio.h>
 #include <string.h>
 
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <mutex>
 #include <string>
 #include <vector>
@@ -1069,6 +1071,198 @@ xhc_status xhc_pre_bwd(const xhc_handle* h, int slot, int64_t T, const xhc_param
     }
     s = join_into(c.st, sd);
     return s == XHC_OK && follow ? wgrad(c.st) : s;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------------------------
+// operators around the connection op
+
+namespace {
+
+// `saved` and `workspace` of the gated feed-forward block
+struct MlpLayout {
+    size_t h, p, q, saved_total;              // saved: bf16 [T][F], then p and q (mlp_pq_bytes each)
+    size_t err, hs, dg, du, ws_total;         // workspace: h of a forward without `saved` where dg is
+};
+
+MlpLayout mlp_layout(int64_t T, int F) {
+    MlpLayout L;
+    const size_t tf = al((size_t)T * F * 2), pq = al(mlp_pq_bytes(T, F));
+    L.h = 0;
+    L.p = tf;
+    L.q = tf + pq;
+    L.saved_total = tf + 2 * pq;
+    L.err = 0;
+    L.hs = L.dg = 256;
+    L.du = L.dg + tf;
+    L.ws_total = L.du + tf;
+    return L;
+}
+
+xhc_status mlp_check(const xhc_mlp_config* c, int64_t T) {
+    if (!c || c->C < 1 || c->F < 1 || c->act < XHC_ACT_SILU || c->act > XHC_ACT_RELU || T <= 0) return XHC_ERR_INVALID_ARG;
+    if (c->C % 8 != 0 || c->F % 8 != 0 || c->C > 16384 || c->F > 65536 || T > (int64_t)1 << 24) return XHC_ERR_UNSUPPORTED;
+    return XHC_OK;
+}
+
+xhc_status norm_check(int N, int C, int64_t T) {
+    if (N < 1 || C < 1 || T <= 0 || T > (int64_t)1 << 30) return XHC_ERR_INVALID_ARG;
+    if (N > MAXN || C % 8 != 0 || C > 16384) return XHC_ERR_UNSUPPORTED;
+    return XHC_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+xhc_status xhc_mlp_saved_bytes(const xhc_mlp_config* cfg, int64_t T, size_t* bytes) {
+    const xhc_status s = mlp_check(cfg, T);
+    if (s != XHC_OK) return s;
+    if (!bytes) return XHC_ERR_INVALID_ARG;
+    *bytes = mlp_layout(T, cfg->F).saved_total;
+    return XHC_OK;
+}
+
+xhc_status xhc_mlp_workspace_bytes(const xhc_mlp_config* cfg, int64_t T, size_t* bytes) {
+    const xhc_status s = mlp_check(cfg, T);
+    if (s != XHC_OK) return s;
+    if (!bytes) return XHC_ERR_INVALID_ARG;
+    *bytes = mlp_layout(T, cfg->F).ws_total;
+    return XHC_OK;
+}
+
+xhc_status xhc_mlp_fwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weights* W, const uint16_t* x, uint16_t* y,
+                       void* saved, void* workspace, void* stream) {
+    const xhc_status s = mlp_check(cfg, T);
+    if (s != XHC_OK) return s;
+    if (!W || !W->gate || !W->up || !W->down || !x || !y || !workspace) return XHC_ERR_INVALID_ARG;
+    if (!aligned16(W->gate) || !aligned16(W->up) || !aligned16(W->down) || !aligned16(x) || !aligned16(y) ||
+        !aligned16(saved) || !aligned16(workspace))
+        return XHC_ERR_ALIGNMENT;
+    const int C = cfg->C, F = cfg->F, T32 = (int)T;
+    const MlpLayout L = mlp_layout(T, F);
+    char *sv = (char*)saved, *ws = (char*)workspace;
+    const cudaStream_t st = (cudaStream_t)stream;
+    PdlScope pdl;
+    pdl.set((size_t)T * (C + F) * 2, st);
+    uint16_t* h = (uint16_t*)(sv ? sv + L.h : ws + L.hs);
+    int* err = (int*)(ws + L.err);
+    XHC_K("mlp_gate", st, launch_mlp_gate(T32, C, F, cfg->act, x, W->gate, W->up, h, sv ? sv + L.p : nullptr,
+                                          sv ? sv + L.q : nullptr, err, st));
+    XHC_K("mlp_down", st, launch_mlp_down(T32, C, F, h, W->down, y, err, st));
+    return XHC_OK;
+}
+
+xhc_status xhc_mlp_bwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weights* W, const uint16_t* x,
+                       const uint16_t* dy, uint16_t* dx, const xhc_mlp_grads* g, int grad_dtype, int accumulate,
+                       const void* saved, void* workspace, void* stream) {
+    const xhc_status s = mlp_check(cfg, T);
+    if (s != XHC_OK) return s;
+    if (!W || !W->gate || !W->up || !W->down || !x || !dy || !dx || !g || !g->gate || !g->up || !g->down || !saved ||
+        !workspace || (grad_dtype != XHC_F32 && grad_dtype != XHC_BF16) || accumulate < 0 || accumulate > 1)
+        return XHC_ERR_INVALID_ARG;
+    if (accumulate && grad_dtype != XHC_F32) return XHC_ERR_UNSUPPORTED;
+    if (!aligned16(W->gate) || !aligned16(W->up) || !aligned16(W->down) || !aligned16(x) || !aligned16(dy) ||
+        !aligned16(dx) || !aligned16(g->gate) || !aligned16(g->up) || !aligned16(g->down) || !aligned16(saved) ||
+        !aligned16(workspace))
+        return XHC_ERR_ALIGNMENT;
+    const int C = cfg->C, F = cfg->F, T32 = (int)T;
+    const MlpLayout L = mlp_layout(T, F);
+    const char* sv = (const char*)saved;
+    char* ws = (char*)workspace;
+    const cudaStream_t st = (cudaStream_t)stream;
+    PdlScope pdl;
+    pdl.set((size_t)T * (C + F) * 2, st);
+    uint16_t *dg = (uint16_t*)(ws + L.dg), *du = (uint16_t*)(ws + L.du);
+    int* err = (int*)(ws + L.err);
+    XHC_K("mlp_dh", st, launch_mlp_dh(T32, C, F, dy, W->down, sv + L.p, sv + L.q, dg, du, err, st));
+    XHC_K("mlp_dx", st, launch_mlp_dx(T32, C, F, dg, du, W->gate, W->up, dx, err, st));
+    XHC_K("mlp_dw", st, launch_mlp_dw(T32, C, F, x, dy, (const uint16_t*)(sv + L.h), dg, du, g->gate, g->up, g->down,
+                                      grad_dtype == XHC_F32, accumulate, err, st));
+    return XHC_OK;
+}
+
+xhc_status xhc_sum_norm_saved_bytes(int N, int C, int64_t T, size_t* bytes) {
+    const xhc_status s = norm_check(N, C, T);
+    if (s != XHC_OK) return s;
+    if (!bytes) return XHC_ERR_INVALID_ARG;
+    *bytes = al((size_t)T * 4) + (N > 1 ? (size_t)T * C * 4 : 0);
+    return XHC_OK;
+}
+
+xhc_status xhc_sum_norm_workspace_bytes(int N, int C, int64_t T, size_t* bytes) {
+    const xhc_status s = norm_check(N, C, T);
+    if (s != XHC_OK) return s;
+    if (!bytes) return XHC_ERR_INVALID_ARG;
+    *bytes = 256 + (size_t)norm_bwd_blocks(T, C) * C * 4;
+    return XHC_OK;
+}
+
+xhc_status xhc_sum_norm_fwd(int N, int C, float eps, int64_t T, const uint16_t* X, const float* w, uint16_t* y,
+                            void* saved, void* stream) {
+    const xhc_status s = norm_check(N, C, T);
+    if (s != XHC_OK) return s;
+    if (!X || !w || !y || !(eps >= 0.f)) return XHC_ERR_INVALID_ARG;
+    if (!aligned16(X) || !aligned16(w) || !aligned16(y) || !aligned16(saved)) return XHC_ERR_ALIGNMENT;
+    const cudaStream_t st = (cudaStream_t)stream;
+    PdlScope pdl;
+    pdl.set((size_t)T * N * C * 2, st);
+    char* sv = (char*)saved;
+    XHC_K("sum_norm", st, launch_norm_fwd((int)T, N, C, eps, X, w, y,
+                                          sv && N > 1 ? (float*)(sv + al((size_t)T * 4)) : nullptr, (float*)sv, st));
+    return XHC_OK;
+}
+
+xhc_status xhc_sum_norm_bwd(int N, int C, int64_t T, const uint16_t* X, const float* w, const uint16_t* dy,
+                            uint16_t* dX, float* dw, int accumulate, const void* saved, void* workspace, void* stream) {
+    const xhc_status s = norm_check(N, C, T);
+    if (s != XHC_OK) return s;
+    if ((N == 1 && !X) || !w || !dy || !dX || !dw || !saved || !workspace || accumulate < 0 || accumulate > 1)
+        return XHC_ERR_INVALID_ARG;
+    if (!aligned16(X) || !aligned16(w) || !aligned16(dy) || !aligned16(dX) || !aligned16(dw) || !aligned16(saved) ||
+        !aligned16(workspace))
+        return XHC_ERR_ALIGNMENT;
+    const cudaStream_t st = (cudaStream_t)stream;
+    PdlScope pdl;
+    pdl.set((size_t)T * N * C * 2, st);
+    const char* sv = (const char*)saved;
+    float* part = (float*)((char*)workspace + 256);
+    XHC_K("sum_norm_bwd", st, launch_norm_bwd((int)T, N, C, X, N > 1 ? (const float*)(sv + al((size_t)T * 4)) : nullptr,
+                                              (const float*)sv, w, dy, dX, part, st));
+    XHC_K("sum_norm_dw", st, launch_norm_dw(norm_bwd_blocks(T, C), C, part, dw, accumulate, st));
+    return XHC_OK;
+}
+
+xhc_status xhc_clip_workspace_bytes(size_t* bytes) {
+    if (!bytes) return XHC_ERR_INVALID_ARG;
+    *bytes = al(clip_workspace());
+    return XHC_OK;
+}
+
+xhc_status xhc_clip_grads(int n, void* const* grads, void* const* out, const int64_t* numel, const int* dtype,
+                          double scale, double max_norm, double eps, float* norm, void* workspace, void* stream) {
+    if (n < 0 || (n > 0 && (!grads || !numel || !dtype)) || !workspace || !std::isfinite(scale) || !(max_norm >= 0.0) ||
+        !(eps >= 0.0) || !std::isfinite(eps))
+        return XHC_ERR_INVALID_ARG;
+    if (n > CLIP_MAX_TENSORS) return XHC_ERR_UNSUPPORTED;
+    size_t bytes = 0;
+    for (int q = 0; q < n; ++q) {
+        if (numel[q] < 0 || (dtype[q] != XHC_F32 && dtype[q] != XHC_BF16)) return XHC_ERR_INVALID_ARG;
+        if (numel[q] > (int64_t)1 << 40) return XHC_ERR_UNSUPPORTED;
+        if (numel[q] == 0) continue;
+        if (!grads[q] || (out && !out[q])) return XHC_ERR_INVALID_ARG;
+        const uintptr_t size = dtype[q] == XHC_F32 ? 4 : 2;
+        if ((uintptr_t)grads[q] % size != 0 || (out && (uintptr_t)out[q] % size != 0)) return XHC_ERR_ALIGNMENT;
+        bytes += (size_t)numel[q] * size;
+    }
+    if (!aligned16(workspace) || ((uintptr_t)norm & 3u) != 0) return XHC_ERR_ALIGNMENT;
+    const cudaStream_t st = (cudaStream_t)stream;
+    PdlScope pdl;
+    pdl.set(bytes, st);
+    const ClipTensors t = {n, grads, out, numel, dtype};
+    XHC_K("clip_grads", st, launch_clip(t, scale, max_norm, eps, norm, (double*)workspace, st));
+    return XHC_OK;
 }
 
 }  // extern "C"

@@ -1,0 +1,236 @@
+// Global norm of many gradient tensors and their scaling:
+//   norm = |scale| sqrt(sum over all tensors of g^2),  out = g * scale * min(1, max_norm / (norm + eps))
+// Both passes are bound by memory.  All tensors form one sequence of 16-byte units, cut into granules of
+// CLIP_G units, one per warp at a time: a warp finds its tensor in the table (a kernel argument: no copy to
+// the device, and a captured graph holds it), so that many small tensors share a launch and its blocks.  The
+// second pass walks the granules from the last to the first: what the first pass read last still lies in L2.
+#include "xhc_internal.cuh"
+
+namespace xhc {
+
+namespace {
+
+constexpr int CLIP_NT = 256;
+constexpr int CLIP_U = 8;              // units a lane has in flight
+constexpr int CLIP_G = 32 * CLIP_U;    // units of a granule
+
+// A table of tensors: tensor q holds units [first[q], first[q + 1]); its granules do not reach over its end, so
+// a granule belongs to one tensor: gran[q] is its first one.
+template <int MAXT>
+struct ClipTable {
+    int n;
+    int64_t gran[MAXT + 1];
+    const void* in[MAXT];
+    void* out[MAXT];
+    int64_t numel[MAXT];    // elements; bit 62: bf16 (else fp32), bit 61: in and out 16-byte aligned
+};
+constexpr int64_t CLIP_BF16 = (int64_t)1 << 62, CLIP_AL = (int64_t)1 << 61;
+
+template <int MAXT>
+__device__ __forceinline__ int clip_find(const ClipTable<MAXT>& tb, const int64_t* gran, int64_t g) {
+    int lo = 0, hi = tb.n;   // gran[lo] <= g < gran[hi]
+    while (hi - lo > 1) {
+        const int m = (lo + hi) >> 1;
+        if (gran[m] <= g) lo = m;
+        else hi = m;
+    }
+    return lo;
+}
+
+// The values of a lane's units of granule `k` of a tensor, zero past its end
+template <bool BF16>
+__device__ __forceinline__ void clip_load(const void* in, int64_t n, bool al, int64_t k, float* v) {
+    constexpr int V = BF16 ? 8 : 4;
+    const int lane = threadIdx.x & 31;
+    const int64_t u0 = k * CLIP_G + lane;
+    if (al && (k + 1) * CLIP_G * V <= n) {
+        uint4 x[CLIP_U];
+#pragma unroll
+        for (int j = 0; j < CLIP_U; ++j) x[j] = ld_stream((const uint4*)in + u0 + 32 * j);
+#pragma unroll
+        for (int j = 0; j < CLIP_U; ++j) {
+            if (BF16) {
+                unpack8(x[j], v + 8 * j);
+            } else {
+                v[4 * j] = __uint_as_float(x[j].x);
+                v[4 * j + 1] = __uint_as_float(x[j].y);
+                v[4 * j + 2] = __uint_as_float(x[j].z);
+                v[4 * j + 3] = __uint_as_float(x[j].w);
+            }
+        }
+    } else {   // a tensor's last granule, or one that is not aligned: element by element
+#pragma unroll
+        for (int j = 0; j < CLIP_U * V; ++j) {
+            const int64_t e = k * CLIP_G * V + 32 * j + lane;
+            v[j] = e < n ? (BF16 ? bf2f(((const uint16_t*)in)[e]) : ((const float*)in)[e]) : 0.f;
+        }
+    }
+}
+
+// The sum of squares of n values: fp32 while no square can leave its range (the sum is of at most 64 terms
+// between 2^-126 and 2^126), else in 64 bits
+template <int n>
+__device__ __forceinline__ double clip_squares(const float* v) {
+    float s = 0.f, m = 0.f;
+#pragma unroll
+    for (int j = 0; j < n; ++j) {
+        s = fmaf(v[j], v[j], s);
+        m = fmaxf(m, fabsf(v[j]));
+    }
+    if (m > 1e-15f && m < 1e17f) return (double)s;   // a NaN among them is in s
+    double d = 0.0;
+#pragma unroll
+    for (int j = 0; j < n; ++j) d = fma((double)v[j], (double)v[j], d);
+    return d;
+}
+
+// Sum over the block's threads, warps in order; thread 0 has it
+__device__ __forceinline__ double clip_block_sum(double v, double* sh) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double t = 0.0;
+    for (int q = 0; q < CLIP_NT / 32; ++q) t += sh[q];
+    return t;
+}
+
+template <int MAXT>
+__device__ __forceinline__ void clip_stage(const ClipTable<MAXT>& tb, int64_t* gran) {
+    for (int q = threadIdx.x; q <= tb.n; q += CLIP_NT) gran[q] = tb.gran[q];
+    __syncthreads();
+}
+
+// part[blockIdx.x] = the block's share of the sum of squares
+template <int MAXT>
+__global__ void __launch_bounds__(CLIP_NT) k_clip_norm(const __grid_constant__ ClipTable<MAXT> tb, double* part) {
+    pdl_entry();
+    __shared__ int64_t gran[MAXT + 1];
+    __shared__ double sh[CLIP_NT / 32];
+    clip_stage(tb, gran);
+    const int64_t total = gran[tb.n], nw = (int64_t)gridDim.x * (CLIP_NT / 32);
+    double sum = 0.0;
+    for (int64_t g = (int64_t)(threadIdx.x >> 5) * gridDim.x + blockIdx.x; g < total; g += nw) {
+        const int q = clip_find(tb, gran, g);
+        const int64_t nm = tb.numel[q], n = nm & (CLIP_AL - 1);
+        float v[CLIP_U * 8];
+        if (nm & CLIP_BF16) {
+            clip_load<true>(tb.in[q], n, (nm & CLIP_AL) != 0, g - gran[q], v);
+            sum += clip_squares<CLIP_U * 8>(v);
+        } else {
+            clip_load<false>(tb.in[q], n, (nm & CLIP_AL) != 0, g - gran[q], v);
+            sum += clip_squares<CLIP_U * 4>(v);
+        }
+    }
+    sum = clip_block_sum(sum, sh);
+    if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+
+template <bool BF16>
+__device__ __forceinline__ void clip_store(const void* in, void* out, int64_t n, bool al, int64_t k, float by) {
+    constexpr int V = BF16 ? 8 : 4;
+    const int lane = threadIdx.x & 31;
+    float v[CLIP_U * V];
+    clip_load<BF16>(in, n, al, k, v);
+#pragma unroll
+    for (int j = 0; j < CLIP_U * V; ++j) v[j] *= by;
+    if (al && (k + 1) * CLIP_G * V <= n) {
+#pragma unroll
+        for (int j = 0; j < CLIP_U; ++j) {
+            uint4* to = (uint4*)out + k * CLIP_G + lane + 32 * j;
+            if (BF16) *to = pack8(v + 8 * j);
+            else *to = make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < CLIP_U * V; ++j) {
+            const int64_t e = k * CLIP_G * V + 32 * j + lane;
+            if (e >= n) continue;
+            if (BF16) ((uint16_t*)out)[e] = f2bf(v[j]);
+            else ((float*)out)[e] = v[j];
+        }
+    }
+}
+
+// Every block adds the np partial sums in the same order, so all use the same factor.
+template <int MAXT>
+__global__ void __launch_bounds__(CLIP_NT) k_clip_scale(const __grid_constant__ ClipTable<MAXT> tb, const double* part,
+                                                        int np, double scale, double max_norm, double eps, float* norm_out) {
+    pdl_entry();
+    __shared__ int64_t gran[MAXT + 1];
+    __shared__ double sh[CLIP_NT / 32];
+    double s = 0.0;
+    for (int q = threadIdx.x; q < np; q += CLIP_NT) s += part[q];
+    s = clip_block_sum(s, sh);
+    clip_stage(tb, gran);
+    const double norm = fabs(scale) * sqrt(s), c = max_norm / (norm + eps);
+    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
+    const float by = (float)(scale * (c >= 1.0 ? 1.0 : c));   // a NaN stays one
+    const int64_t total = gran[tb.n], nw = (int64_t)gridDim.x * (CLIP_NT / 32);
+    for (int64_t g = total - 1 - ((int64_t)(threadIdx.x >> 5) * gridDim.x + blockIdx.x); g >= 0; g -= nw) {
+        const int q = clip_find(tb, gran, g);
+        if (by == 1.0f && tb.in[q] == tb.out[q]) continue;   // in place: nothing to change
+        const int64_t nm = tb.numel[q], n = nm & (CLIP_AL - 1);
+        if (nm & CLIP_BF16) clip_store<true>(tb.in[q], tb.out[q], n, (nm & CLIP_AL) != 0, g - gran[q], by);
+        else clip_store<false>(tb.in[q], tb.out[q], n, (nm & CLIP_AL) != 0, g - gran[q], by);
+    }
+}
+
+constexpr int CLIP_SMALL = 100, CLIP_LARGE = 900;   // tensors of a launch: 3.2 KB and 28.8 KB of arguments
+
+template <int MAXT>
+struct ClipPass {
+    ClipTable<MAXT> tb;
+    int grid;
+};
+
+// Tensors [q0, q1) as a table, and its blocks: what the GPU holds at once, but no more than there are granules
+template <int MAXT>
+int clip_fill(ClipTable<MAXT>& tb, const ClipTensors& t, int q0, int q1) {
+    tb.n = q1 - q0;
+    int64_t g = 0;
+    for (int q = q0; q < q1; ++q) {
+        const int k = q - q0;
+        const bool bf = t.dtype[q] == XHC_BF16;
+        const void* in = t.in[q];
+        void* out = t.out ? t.out[q] : const_cast<void*>(t.in[q]);
+        tb.gran[k] = g;
+        tb.in[k] = in;
+        tb.out[k] = out;
+        tb.numel[k] = t.numel[q] | (bf ? CLIP_BF16 : 0) | ((((uintptr_t)in | (uintptr_t)out) & 15u) == 0 ? CLIP_AL : 0);
+        const int64_t per = (int64_t)CLIP_G * (bf ? 8 : 4);
+        g += (t.numel[q] + per - 1) / per;
+    }
+    tb.gran[tb.n] = g;
+    const int64_t most = (int64_t)device_sms() * CLIP_BLOCKS_SM, want = (g + CLIP_NT / 32 - 1) / (CLIP_NT / 32);
+    return (int)(want < 1 ? 1 : want < most ? want : most);
+}
+
+template <int MAXT>
+cudaError_t clip_run(const ClipTensors& t, double scale, double max_norm, double eps, float* norm_out, double* part,
+                     cudaStream_t st) {
+    int np = 0;
+    ClipTable<MAXT> tb;
+    for (int q = 0; q < t.n || q == 0; q += MAXT) {
+        const int grid = clip_fill(tb, t, q, t.n < q + MAXT ? t.n : q + MAXT);
+        XHC_LAUNCH(st, grid, CLIP_NT, 0, (k_clip_norm<MAXT>), tb, part + np);
+        np += grid;
+    }
+    for (int q = 0; q < t.n || q == 0; q += MAXT) {
+        const int grid = clip_fill(tb, t, q, t.n < q + MAXT ? t.n : q + MAXT);
+        XHC_LAUNCH(st, grid, CLIP_NT, 0, (k_clip_scale<MAXT>), tb, part, np, scale, max_norm, eps, q == 0 ? norm_out : nullptr);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t clip_workspace() { return (size_t)(CLIP_MAX_TENSORS / CLIP_LARGE) * device_sms() * CLIP_BLOCKS_SM * sizeof(double); }
+
+cudaError_t launch_clip(const ClipTensors& t, double scale, double max_norm, double eps, float* norm_out, double* part,
+                        cudaStream_t st) {
+    if (t.n <= CLIP_SMALL) return clip_run<CLIP_SMALL>(t, scale, max_norm, eps, norm_out, part, st);
+    return clip_run<CLIP_LARGE>(t, scale, max_norm, eps, norm_out, part, st);
+}
+
+}  // namespace xhc

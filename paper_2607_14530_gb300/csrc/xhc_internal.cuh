@@ -712,4 +712,42 @@ cudaError_t launch_full_dx(const Dims& d, int T, const float* dz, const WSegs& W
                            const int* I, const float* dxact, const float* scal,
                            uint16_t* dX, cudaStream_t st);
 
+// ---- operators around the connection op ----
+// y = w s / sqrt(mean s^2 + eps) with s the sum of a token's N streams; sum [T][C] and rstd [T] null: not kept
+cudaError_t launch_norm_fwd(int T, int N, int C, float eps, const uint16_t* X, const float* w, uint16_t* y,
+                            float* sum, float* rstd, cudaStream_t st);
+int norm_bwd_blocks(int64_t T, int C);
+// part [norm_bwd_blocks][C]: the blocks' parts of dw, added up by launch_norm_dw; sum null: X is it (N = 1)
+cudaError_t launch_norm_bwd(int T, int N, int C, const uint16_t* X, const float* sum, const float* rstd, const float* w,
+                            const uint16_t* dy, uint16_t* dX, float* part, cudaStream_t st);
+cudaError_t launch_norm_dw(int P, int C, const float* part, float* dw, int accumulate, cudaStream_t st);
+
+constexpr int CLIP_MAX_TENSORS = 45000;
+constexpr int CLIP_BLOCKS_SM = 4;
+struct ClipTensors {
+    int n;
+    void* const* in;
+    void* const* out;   // null: in place
+    const int64_t* numel;
+    const int* dtype;
+};
+size_t clip_workspace();
+cudaError_t launch_clip(const ClipTensors& t, double scale, double max_norm, double eps, float* norm_out, double* part,
+                        cudaStream_t st);
+
+// bytes of p (and of q) of the gated feed-forward block
+size_t mlp_pq_bytes(int64_t T, int F);
+// h = q u, p = u act'(g), q = act(g); p null: only h
+cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, const uint16_t* Wg, const uint16_t* Wu,
+                            uint16_t* h, void* p, void* q, int* err, cudaStream_t st);
+cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, int* err,
+                            cudaStream_t st);
+cudaError_t launch_mlp_dh(int T, int C, int F, const uint16_t* dy, const uint16_t* Wd, const void* p, const void* q,
+                          uint16_t* dg, uint16_t* du, int* err, cudaStream_t st);
+cudaError_t launch_mlp_dx(int T, int C, int F, const uint16_t* dg, const uint16_t* du, const uint16_t* Wg,
+                          const uint16_t* Wu, uint16_t* dx, int* err, cudaStream_t st);
+cudaError_t launch_mlp_dw(int T, int C, int F, const uint16_t* x, const uint16_t* dy, const uint16_t* h,
+                          const uint16_t* dg, const uint16_t* du, void* dWg, void* dWu, void* dWd, int f32,
+                          int accumulate, int* err, cudaStream_t st);
+
 }  // namespace xhc

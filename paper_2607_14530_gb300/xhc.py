@@ -50,6 +50,14 @@ class _SavedLayout(ctypes.Structure):
                 ("xact", ctypes.c_size_t), ("zfull", ctypes.c_size_t), ("stats", ctypes.c_size_t)]
 
 
+class _MlpConfig(ctypes.Structure):
+    _fields_ = [("C", ctypes.c_int), ("F", ctypes.c_int), ("act", ctypes.c_int)]
+
+
+class _MlpWeights(ctypes.Structure):
+    _fields_ = [("gate", _P), ("up", _P), ("down", _P)]   # and xhc_mlp_grads
+
+
 class XhcError(RuntimeError):
     pass
 
@@ -88,6 +96,18 @@ def lib() -> ctypes.CDLL:
         L.xhc_halo_add.argtypes = [vp, i64, i64, vp, vp, vp]
         L.xhc_post_fwd_halo.argtypes = [vp, ctypes.c_int, i64, P, vp, vp, vp, vp, vp, vp]
         L.xhc_post_bwd_halo.argtypes = [vp, ctypes.c_int, i64, P, vp, vp, vp, vp, P, vp, vp, vp, vp, vp]
+        M, W, f64, f32 = ctypes.POINTER(_MlpConfig), ctypes.POINTER(_MlpWeights), ctypes.c_double, ctypes.c_float
+        ci = ctypes.c_int
+        L.xhc_mlp_saved_bytes.argtypes = [M, i64, ctypes.POINTER(sz)]
+        L.xhc_mlp_workspace_bytes.argtypes = [M, i64, ctypes.POINTER(sz)]
+        L.xhc_mlp_fwd.argtypes = [M, i64, W, vp, vp, vp, vp, vp]
+        L.xhc_mlp_bwd.argtypes = [M, i64, W, vp, vp, vp, W, ci, ci, vp, vp, vp]
+        L.xhc_sum_norm_saved_bytes.argtypes = [ci, ci, i64, ctypes.POINTER(sz)]
+        L.xhc_sum_norm_workspace_bytes.argtypes = [ci, ci, i64, ctypes.POINTER(sz)]
+        L.xhc_sum_norm_fwd.argtypes = [ci, ci, f32, i64, vp, vp, vp, vp, vp]
+        L.xhc_sum_norm_bwd.argtypes = [ci, ci, i64, vp, vp, vp, vp, vp, ci, vp, vp, vp]
+        L.xhc_clip_workspace_bytes.argtypes = [ctypes.POINTER(sz)]
+        L.xhc_clip_grads.argtypes = [ci, vp, vp, vp, vp, f64, f64, f64, vp, vp, vp]
         L.xhc_workspace_error.argtypes = [vp, ctypes.POINTER(ctypes.c_int), ctypes.c_int]
         L.xhc_debug_set.argtypes = [ctypes.c_int, i64]
         L.xhc_trace_enable.argtypes = [ctypes.c_int]
@@ -530,3 +550,244 @@ class Group:
             self.post_bwd(t, pp, X, dX, outs[t], d_outs[t], gg, saved, ws, stream)
             self.pre_bwd(t, pp, X, d_inputs[t], dX, gg, saved, ws, stream)
         return d_outs
+
+
+# ---- operators around the connection op ----
+
+
+def _arg(t, name, dtype, shape=None):
+    """The pointer of an operand: contiguous, of that type and shape, on the current CUDA device."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        raise XhcError(f"{name} must be a contiguous {str(dtype)[6:]} CUDA tensor")
+    if shape is not None and tuple(t.shape) != shape:
+        raise XhcError(f"{name} must be of shape {list(shape)}, got {list(t.shape)}")
+    if t.device.index != torch.cuda.current_device():
+        raise XhcError(f"{name} is on cuda:{t.device.index}, which is not the current device")
+    return t.data_ptr()
+
+
+def _buffer(t, name, nbytes):
+    """The pointer of a `saved` or `workspace` buffer (uint8, at least nbytes)."""
+    p = _arg(t, name, torch.uint8)
+    if t.numel() < nbytes:
+        raise XhcError(f"{name} has {t.numel()} bytes, {nbytes} are needed")
+    return p
+
+
+class Mlp:
+    """The gated feed-forward block y = (act(x W_gate^T) * (x W_up^T)) W_down^T (xhc_mlp_fwd, xhc_mlp_bwd):
+    the MLP sublayer between a group's pre_fwd and post_fwd.
+
+    Weights ``{"W_gate": [F, C], "W_up": [F, C], "W_down": [C, F]}`` and activations are bf16; weight
+    gradients, under the same names, fp32 (written, or added to with ``accumulate``) or bf16 (written)."""
+
+    ACTS = {"silu": 0, "gelu": 1, "relu": 2}
+
+    def __init__(self, C: int, F: int, act: str = "silu"):
+        if act not in self.ACTS:
+            raise XhcError(f"unknown activation {act!r}: one of {', '.join(self.ACTS)}")
+        self.C, self.F, self.act = C, F, act
+        self._c = _MlpConfig(C, F, self.ACTS[act])
+        self._sizes = {}
+        self.saved_bytes(1)   # the widths are checked here
+
+    def _bytes(self, T: int) -> tuple:
+        """(saved, workspace) bytes of T tokens."""
+        got = self._sizes.get(T)
+        if got is None:
+            a, b = ctypes.c_size_t(), ctypes.c_size_t()
+            _check(lib().xhc_mlp_saved_bytes(ctypes.byref(self._c), T, ctypes.byref(a)), "xhc_mlp_saved_bytes")
+            _check(lib().xhc_mlp_workspace_bytes(ctypes.byref(self._c), T, ctypes.byref(b)), "xhc_mlp_workspace_bytes")
+            if len(self._sizes) >= 4096:
+                self._sizes.clear()
+            got = self._sizes[T] = (a.value, b.value)
+        return got
+
+    def saved_bytes(self, T: int) -> int:
+        return self._bytes(T)[0]
+
+    def workspace_bytes(self, T: int) -> int:
+        return self._bytes(T)[1]
+
+    def alloc_saved(self, T: int, device="cuda"):
+        """A `saved` buffer: one per forward whose backward is still to come."""
+        return torch.empty(self.saved_bytes(T), dtype=torch.uint8, device=device)
+
+    def alloc_workspace(self, T: int, device="cuda"):
+        """A `workspace` buffer (scratch of one call at a time), error word zeroed."""
+        ws = torch.empty(self.workspace_bytes(T), dtype=torch.uint8, device=device)
+        ws[:256].zero_()
+        return ws
+
+    def shapes(self) -> dict:
+        return {"W_gate": (self.F, self.C), "W_up": (self.F, self.C), "W_down": (self.C, self.F)}
+
+    def _weights(self, d: dict, what: str, dtype) -> _MlpWeights:
+        C, F = self.C, self.F
+        return _MlpWeights(_arg(d.get("W_gate"), what + "W_gate", dtype, (F, C)), _arg(d.get("W_up"), what + "W_up", dtype, (F, C)),
+                           _arg(d.get("W_down"), what + "W_down", dtype, (C, F)))
+
+    def forward(self, P: dict, x, ws, saved=None, y=None, stream=None):
+        """y [T, C] of x [T, C].  ``saved``: what the backward needs is kept there (None: no backward)."""
+        bf, T = torch.bfloat16, x.shape[0]
+        px = _arg(x, "x", bf, (T, self.C))
+        if y is None:
+            y = torch.empty_like(x)
+        nsaved, nws = self._bytes(T)
+        W = self._weights(P, "", bf)
+        _check(lib().xhc_mlp_fwd(self._c, T, W, px, _arg(y, "y", bf, (T, self.C)),
+                                 None if saved is None else _buffer(saved, "saved", nsaved), _buffer(ws, "ws", nws),
+                                 _stream(stream)), "xhc_mlp_fwd")
+        return y
+
+    def backward(self, P: dict, x, dy, grads: dict, saved, ws, dx=None, accumulate=False, stream=None):
+        """dx [T, C]; the weight gradients go into ``grads``."""
+        bf, T = torch.bfloat16, x.shape[0]
+        px = _arg(x, "x", bf, (T, self.C))
+        if dx is None:
+            dx = torch.empty_like(x)
+        nsaved, nws = self._bytes(T)
+        W = self._weights(P, "", bf)
+        gt = getattr(grads.get("W_gate"), "dtype", None)
+        if gt not in (torch.float32, bf):
+            raise XhcError("weight gradients must be fp32 or bf16 CUDA tensors")
+        if accumulate and gt is bf:
+            raise XhcError("bf16 weight gradients are written, not accumulated: use fp32 ones")
+        _check(lib().xhc_mlp_bwd(self._c, T, W, px, _arg(dy, "dy", bf, (T, self.C)), _arg(dx, "dx", bf, (T, self.C)),
+                                 self._weights(grads, "gradient of ", gt), 1 if gt is bf else 0, 1 if accumulate else 0,
+                                 _buffer(saved, "saved", nsaved), _buffer(ws, "ws", nws), _stream(stream)), "xhc_mlp_bwd")
+        return dx
+
+
+class SumNorm:
+    """RMS norm of the sum of a token's N streams, y = w s / sqrt(mean(s^2) + eps), s = sum_i X[t][i]
+    (xhc_sum_norm_fwd, xhc_sum_norm_bwd): the final reduction of a stack, or with N = 1 the norm at a
+    sublayer's entry.  X [T, N, C] (N = 1: or [T, C]) and y [T, C] bf16, w [C] fp32."""
+
+    def __init__(self, N: int, C: int, eps: float = 1e-5):
+        if not 0.0 <= eps < float("inf"):
+            raise XhcError("eps must be finite and not negative")
+        self.N, self.C, self.eps = N, C, eps
+        self._sizes = {}
+        self.saved_bytes(1)   # N and C are checked here
+
+    def _bytes(self, T: int) -> tuple:
+        """(saved, workspace) bytes of T tokens."""
+        got = self._sizes.get(T)
+        if got is None:
+            a, b = ctypes.c_size_t(), ctypes.c_size_t()
+            _check(lib().xhc_sum_norm_saved_bytes(self.N, self.C, T, ctypes.byref(a)), "xhc_sum_norm_saved_bytes")
+            _check(lib().xhc_sum_norm_workspace_bytes(self.N, self.C, T, ctypes.byref(b)), "xhc_sum_norm_workspace_bytes")
+            if len(self._sizes) >= 4096:
+                self._sizes.clear()
+            got = self._sizes[T] = (a.value, b.value)
+        return got
+
+    def saved_bytes(self, T: int) -> int:
+        return self._bytes(T)[0]
+
+    def workspace_bytes(self, T: int) -> int:
+        return self._bytes(T)[1]
+
+    def alloc_saved(self, T: int, device="cuda"):
+        return torch.empty(self.saved_bytes(T), dtype=torch.uint8, device=device)
+
+    def alloc_workspace(self, T: int, device="cuda"):
+        """Scratch of the backward."""
+        return torch.empty(self.workspace_bytes(T), dtype=torch.uint8, device=device)
+
+    def _state(self, t, name, T):
+        return _arg(t, name, torch.bfloat16, (T, self.C) if self.N == 1 and t.dim() == 2 else (T, self.N, self.C))
+
+    def forward(self, w, X, y=None, saved=None, stream=None):
+        bf, T = torch.bfloat16, X.shape[0]
+        pX = self._state(X, "X", T)
+        if y is None:
+            y = torch.empty(T, self.C, dtype=bf, device=X.device)
+        _check(lib().xhc_sum_norm_fwd(self.N, self.C, self.eps, T, pX, _arg(w, "w", torch.float32, (self.C,)),
+                                      _arg(y, "y", bf, (T, self.C)),
+                                      None if saved is None else _buffer(saved, "saved", self._bytes(T)[0]), _stream(stream)),
+               "xhc_sum_norm_fwd")
+        return y
+
+    def backward(self, w, X, dy, dw, saved, ws, dX=None, accumulate=False, stream=None):
+        """dX, shaped like X (with N > 1 X is not read and may be None); dw [C] fp32 is written, or
+        added to with ``accumulate``."""
+        T = dy.shape[0]
+        if X is None and self.N == 1:
+            raise XhcError("X is needed with N = 1")
+        pX = None if X is None else self._state(X, "X", T)
+        if dX is None:
+            dX = torch.empty((T, self.N, self.C) if X is None else X.shape, dtype=torch.bfloat16, device=dy.device)
+        nsaved, nws = self._bytes(T)
+        _check(lib().xhc_sum_norm_bwd(self.N, self.C, T, pX, _arg(w, "w", torch.float32, (self.C,)),
+                                      _arg(dy, "dy", torch.bfloat16, (T, self.C)), self._state(dX, "dX", T),
+                                      _arg(dw, "dw", torch.float32, (self.C,)), 1 if accumulate else 0,
+                                      _buffer(saved, "saved", nsaved), _buffer(ws, "ws", nws), _stream(stream)),
+               "xhc_sum_norm_bwd")
+        return dX
+
+
+_clip_bytes = None
+
+
+def clip_workspace(device="cuda"):
+    """A `workspace` buffer of clip_grads (scratch of one call at a time)."""
+    global _clip_bytes
+    if _clip_bytes is None:
+        n = ctypes.c_size_t()
+        _check(lib().xhc_clip_workspace_bytes(ctypes.byref(n)), "xhc_clip_workspace_bytes")
+        _clip_bytes = n.value
+    return torch.empty(_clip_bytes, dtype=torch.uint8, device=device)
+
+
+def clip_grads(grads, max_norm: float, scale: float = 1.0, eps: float = 1e-6, out=None, norm=None, ws=None, stream=None):
+    """The global norm of all gradients times ``scale``, and every gradient times
+    scale * min(1, max_norm / (norm + eps)) (xhc_clip_grads).
+
+    ``grads``: a list or dict of contiguous fp32 or bf16 CUDA tensors (None entries are passed over), each
+    once; ``out``: where the results go, alike (None: in place).  Returns the norm (fp32 [1], on the device:
+    nothing waits for it).  ``max_norm`` infinite: only measured and scaled."""
+    if isinstance(grads, dict):
+        names = list(grads)
+        if out is not None:
+            if not isinstance(out, dict) or set(out) != set(names):
+                raise XhcError("out must have the names of grads")
+            out = [out[n] for n in names]
+        grads = [grads[n] for n in names]
+    else:
+        grads = list(grads)
+        if out is not None:
+            out = list(out)
+            if len(out) != len(grads):
+                raise XhcError(f"{len(grads)} gradients and {len(out)} outputs")
+    if out is not None:
+        for q, (g, o) in enumerate(zip(grads, out)):
+            if (g is None) != (o is None) or (g is not None and (o.dtype is not g.dtype or o.shape != g.shape)):
+                raise XhcError(f"out[{q}] must be like its gradient")
+        out = [o for o in out if o is not None]
+    grads = [g for g in grads if g is not None]
+    n, device = len(grads), torch.cuda.current_device()
+    for what, ts in (("gradient", grads), ("output", out or ())):
+        for q, t in enumerate(ts):
+            if t.dtype not in (torch.float32, torch.bfloat16) or not t.is_cuda or not t.is_contiguous():
+                raise XhcError(f"{what} {q} must be a contiguous fp32 or bf16 CUDA tensor")
+            if t.device.index != device:
+                raise XhcError(f"{what} {q} is on cuda:{t.device.index}, which is not the current device")
+    ptrs = [t.data_ptr() for t in (grads if out is None else out)]
+    nonempty = [p for p, t in zip(ptrs, grads) if t.numel()]
+    if len(set(nonempty)) != len(nonempty):
+        raise XhcError("the same tensor is there twice")
+    I = ctypes.c_int64 * n
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device="cuda")
+    if ws is None:
+        ws = clip_workspace()
+    elif _clip_bytes is None:
+        clip_workspace("cpu")
+    _check(lib().xhc_clip_grads(n, I(*[t.data_ptr() for t in grads]), None if out is None else I(*ptrs),
+                                I(*[t.numel() for t in grads]),
+                                (ctypes.c_int * n)(*[1 if t.dtype is torch.bfloat16 else 0 for t in grads]),
+                                scale, max_norm, eps, _arg(norm, "norm", torch.float32, (1,)), _buffer(ws, "ws", _clip_bytes),
+                                _stream(stream)), "xhc_clip_grads")
+    return norm

@@ -1,0 +1,126 @@
+"""Plain 64-bit forms of the operators around the connection op, with bounds on what the kernels' roundings
+can change.
+
+A rounding to bf16 is off by at most 2^-8 of the value (half a step; 2^-9 on average over a binade's
+upper end, never more than 2^-8), one to fp32 by 2^-24.  The bounds below add those up for the roundings that
+the operators document; fp32 sums of n terms are off by at most n 2^-24 of the sum of their magnitudes,
+taken as n 2^-23 for the tensor cores' own order of summation."""
+from __future__ import annotations
+
+import math
+
+import torch
+
+F64 = torch.float64
+BF = 2.0 ** -8
+F32 = 2.0 ** -23
+
+
+def act(g, name):
+    """The activation and its derivative."""
+    if name == "silu":
+        s = torch.sigmoid(g)
+        return g * s, s * (1 + g * (1 - s))
+    if name == "gelu":
+        c = torch.special.ndtr(g)
+        return g * c, c + g * torch.exp(-0.5 * g * g) / math.sqrt(2 * math.pi)
+    on = (g > 0).to(g.dtype)
+    return torch.where(g > 0, g, torch.zeros_like(g)), on
+
+
+def mlp(x, P, name, dy=None):
+    """The gated feed-forward block in 64 bits: {"y", and with dy "dx", "W_gate", "W_up", "W_down"}, and
+    under "bound" how far the kernels' results may be, element by element, before their own last rounding."""
+    x, Wg, Wu, Wd = x.to(F64), P["W_gate"].to(F64), P["W_up"].to(F64), P["W_down"].to(F64)
+    T, C = x.shape
+    F = Wg.shape[0]
+    g, u = x @ Wg.T, x @ Wu.T
+    q, dq = act(g, name)
+    h, p = q * u, u * dq
+    # fp32 sums of g and u; the activations have slopes of at most 1.13, and ~8 fp32 roundings of their own
+    eg, eu = C * F32 * (x.abs() @ Wg.abs().T), C * F32 * (x.abs() @ Wu.abs().T)
+    eq = 1.13 * eg + 16 * F32 * q.abs()
+    eh = BF * h.abs() + 1.01 * (eq * u.abs() + q.abs() * eu)
+    out = {"y": h @ Wd.T}
+    bound = {"y": eh @ Wd.abs().T + F * F32 * (h.abs() @ Wd.abs().T)}
+    if dy is not None:
+        dy = dy.to(F64)
+        dh = dy @ Wd
+        dg, du = dh * p, dh * q
+        out.update(dx=dg @ Wg + du @ Wu, W_gate=dg.T @ x, W_up=du.T @ x, W_down=dy.T @ h)
+        edh = C * F32 * (dy.abs() @ Wd.abs())
+        # act'' is at most 1 (silu 0.5, gelu 0.8); relu's slope jumps where g may have either sign
+        ep = BF * p.abs() + u.abs() * (eg + 16 * F32) + eu * dq.abs()
+        if name == "relu":
+            ep = ep + u.abs() * (g.abs() <= eg)
+        edg = 1.01 * (BF * dg.abs() + dh.abs() * ep + edh * p.abs())
+        edu = 1.01 * (BF * du.abs() + dh.abs() * (BF * q.abs() + eq) + edh * q.abs())
+        ax = x.abs()
+        bound["dx"] = edg @ Wg.abs() + edu @ Wu.abs() + 2 * F * F32 * (dg.abs() @ Wg.abs() + du.abs() @ Wu.abs())
+        bound["W_gate"] = edg.T @ ax + T * F32 * (dg.abs().T @ ax)
+        bound["W_up"] = edu.T @ ax + T * F32 * (du.abs().T @ ax)
+        bound["W_down"] = dy.abs().T @ eh + T * F32 * (dy.abs().T @ h.abs())
+    out["bound"] = bound
+    return out
+
+
+# roundings to bf16 on the way to a result (its own last one included): their errors, each at most 2^-8
+# of its value and of either sign, add up as a root of squares in the 2-norm
+MLP_ROUNDINGS = {"y": 2, "dx": 3, "W_gate": 3, "W_up": 3, "W_down": 2}
+
+
+def assert_mlp(got, ref, names=None):
+    for n in names or got:
+        g, r, b = got[n].detach().to("cpu", F64), ref[n].cpu(), ref["bound"][n].cpu()
+        assert g.shape == r.shape, n
+        last = BF if got[n].dtype == torch.bfloat16 else F32
+        over = (g - r).abs() - (b + last * (r.abs() + b) + 1e-37)
+        assert bool((over <= 0).all()), f"{n}: {int((over > 0).sum())} of {over.numel()} over the bound, by up to {float(over.max()):.3e}"
+        rel = float((g - r).norm() / r.norm().clamp(min=1e-30))
+        assert rel <= math.sqrt(MLP_ROUNDINGS[n]) * BF, f"{n}: relative 2-norm {rel:.3e}"
+
+
+def sum_norm(X, w, eps, dy=None):
+    """RMS norm of the sum of the streams in 64 bits: {"y", "dX", "dw"} and "bound" as above."""
+    X, w = X.to(F64), w.to(F64)
+    if X.dim() == 2:
+        X = X[:, None]
+    T, N, C = X.shape
+    s = X.sum(1)
+    r = 1 / torch.sqrt((s * s).mean(1, keepdim=True) + eps)
+    n = s * r
+    out = {"y": n * w}
+    es = N * F32 * X.abs().sum(1)                       # fp32 sum of the streams
+    rr = C * F32 + r * r * (s.abs() * es).mean(1, keepdim=True) + 4 * F32   # relative, of r
+    en = es * r + n.abs() * rr
+    bound = {"y": 1.01 * (en * w.abs() + 2 * F32 * out["y"].abs())}
+    if dy is not None:
+        dy = dy.to(F64)
+        d = dy * w
+        m = (d * n).mean(1, keepdim=True)
+        out["dX"] = (r * (d - n * m))[:, None].expand(T, N, C)
+        out["dw"] = (dy * n).sum(0)
+        em = (d.abs() * en).mean(1, keepdim=True) + C * F32 * (d * n).abs().mean(1, keepdim=True)
+        eds = r * (rr * (d.abs() + (n * m).abs()) + en * m.abs() + n.abs() * em + 4 * F32 * (d.abs() + (n * m).abs()))
+        bound["dX"] = (1.01 * eds)[:, None].expand(T, N, C)
+        bound["dw"] = 1.01 * ((dy.abs() * en).sum(0) + T * F32 * (dy * n).abs().sum(0))
+    out["bound"] = bound
+    return out
+
+
+def assert_within(got, ref, names=None):
+    """Element by element within the bound and the result's own rounding."""
+    for n in names or got:
+        g, r, b = got[n].detach().to("cpu", F64), ref[n].cpu(), ref["bound"][n].cpu()
+        g = g.reshape(r.shape)
+        last = BF if got[n].dtype == torch.bfloat16 else F32
+        over = (g - r).abs() - (b + last * (r.abs() + b) + 1e-37)
+        assert bool((over <= 0).all()), f"{n}: {int((over > 0).sum())} of {over.numel()} over the bound, by up to {float(over.max()):.3e}"
+
+
+def clip(grads, max_norm, scale=1.0, eps=1e-6):
+    """(norm, factor, the gradients times it) in 64 bits."""
+    total = math.fsum(float(g.to(F64).square().sum()) if g.numel() else 0.0 for g in grads)
+    norm = abs(scale) * math.sqrt(total)
+    by = scale * min(1.0, max_norm / (norm + eps)) if norm + eps > 0 else scale
+    return norm, by, [g.to(F64) * by for g in grads]

@@ -1,0 +1,161 @@
+"""The global gradient norm and clipping against its 64-bit form."""
+import math
+
+import pytest
+import torch
+
+import op_refs as R
+from paper_2607_14530_gb300.xhc import Config, XhcError, clip_grads, clip_workspace
+from xhc_cases import Guarded
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+INF = float("inf")
+
+
+def tensors(sizes, seed=0, std=1.0, dtypes=(F32, BF)):
+    g = torch.Generator().manual_seed(seed)
+    return [(torch.randn(n, generator=g) * std * 10.0 ** -(i % 3)).to(dtypes[i % len(dtypes)]) for i, n in enumerate(sizes)]
+
+
+def check(host, max_norm, scale=1.0, in_place=False, offset=0):
+    """clip_grads of copies of `host` inside guard bands, `offset` elements off a 16-byte boundary."""
+    def at(t):
+        pad = torch.zeros(offset, dtype=t.dtype)
+        gd = Guarded(torch.cat([pad, t.reshape(-1), pad]))
+        return gd, gd.t[offset:offset + t.numel()].view(t.shape)
+
+    ins = [at(t) for t in host]
+    outs = ins if in_place else [at(torch.full_like(t, float("nan"))) for t in host]
+    norm = clip_grads([v for _, v in ins], max_norm, scale=scale, out=None if in_place else [v for _, v in outs])
+    torch.cuda.synchronize()
+    want, by, ref = R.clip(host, max_norm, scale)
+    # 64-bit sums of exact squares, or fp32 sums of at most 64 of them (64 2^-24 of each at most); the root halves that
+    assert math.isclose(float(norm), want, rel_tol=2.0 ** -18, abs_tol=1e-45), (float(norm), want)
+    for (gd, v), r, h in zip(outs, ref, host):
+        assert gd.intact()
+        last = R.BF if v.dtype is BF else R.F32
+        over = (v.cpu().double() - r).abs() - (2.0 ** -18 + last) * r.abs() - (2.0 ** -133 if v.dtype is BF else 2.0 ** -149)
+        assert bool((over <= 0).all()), float(over.max())
+        if offset:
+            assert bool((gd.t[:offset] == 0).all()) and bool((gd.t[-offset:] == 0).all())
+    if not in_place:
+        for (gd, v), h in zip(ins, host):
+            assert gd.intact() and torch.equal(v.cpu(), h)
+    return float(norm)
+
+
+SIZES = [1, 3, 4, 7, 8, 255, 256, 1023, 1024, 1025, 2047, 2048, 2049, 5000, 0, 65536, 100003]
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("offset", [0, 1, 3, 4, 8])
+@pytest.mark.parametrize("bound", [0.5, 1e9])
+def test_sizes_types_and_alignments(in_place, offset, bound):
+    check(tensors(SIZES, seed=offset), bound, in_place=in_place, offset=offset)
+
+
+@pytest.mark.parametrize("scale", [0.25, 1 / 3, -2.0, 0.0, 1e-20])
+@pytest.mark.parametrize("bound", [0.5, 1e9, 0.0, INF])
+def test_scales_and_bounds(scale, bound):
+    check(tensors(SIZES[:8], seed=1), bound, scale)
+
+
+@pytest.mark.parametrize("count", [1, 2, 99, 100, 101, 900, 901, 2000])
+def test_many_tensors(count):
+    """On both sides of a launch's table, and over several launches."""
+    check(tensors([1 + 37 * i % 300 for i in range(count)], seed=count), 0.1)
+
+
+def test_one_large_tensor_and_more_work_than_blocks():
+    check(tensors([40_000_003, 5, 20_000_000], seed=2), 1.0)
+
+
+@pytest.mark.parametrize("std", [1e-30, 1e-22, 1e-12, 1e12, 1e22, 1e30, 1e36])
+def test_squares_beyond_fp32(std):
+    """Squares that fp32 cannot hold, alone and beside ordinary values."""
+    check(tensors([1000, 5000], seed=3, std=std), 1.0)
+    check(tensors([1000, 5000], seed=3, std=std) + tensors([777], seed=4), 1.0)
+
+
+def test_nothing_to_clip_keeps_the_bits():
+    host = tensors(SIZES, seed=5)
+    dev = [t.cuda() for t in host]
+    norm = clip_grads(dev, INF)
+    assert math.isclose(float(norm), R.clip(host, INF)[0], rel_tol=2.0 ** -18)
+    assert all(torch.equal(a.cpu(), b) for a, b in zip(dev, host))
+    clip_grads(dev, 1e9)
+    assert all(torch.equal(a.cpu(), b) for a, b in zip(dev, host))
+    assert float(clip_grads([], 1.0)) == 0.0
+    assert float(clip_grads([torch.zeros(100, device="cuda")], 1.0)) == 0.0
+
+
+def test_values_that_are_not_finite():
+    for bad, factor in ((float("nan"), float("nan")), (INF, 0.0)):
+        dev = [t.cuda() for t in tensors([100, 3000], seed=6)]
+        dev[1][2500] = bad
+        norm = float(clip_grads(dev, 1.0))
+        assert math.isnan(norm) if math.isnan(bad) else norm == INF
+        assert bool(dev[1][2500].isnan())
+        rest = torch.cat([dev[0].float(), dev[1][:2500].float()])
+        assert bool(rest.isnan().all()) if math.isnan(factor) else bool((rest == 0).all())
+
+
+def test_names_and_missing_gradients():
+    cfg = Config.flash(8, 4, 2, 256, 4)
+    gen = torch.Generator().manual_seed(7)
+    host = {n: torch.randn(s, generator=gen) for n, s in cfg.param_shapes().items()}
+    dev = {n: v.cuda() for n, v in host.items()}
+    dev["none"] = None
+    norm = clip_grads(dev, 2.0)
+    want, by, ref = R.clip(list(host.values()), 2.0)
+    assert math.isclose(float(norm), want, rel_tol=2.0 ** -18)
+    for n, r in zip(host, ref):
+        assert bool(((dev[n].cpu().double() - r).abs() <= 2.0 ** -17 * r.abs()).all()), n
+
+
+def test_streams_repeats_and_graphs():
+    host = tensors([65536, 1000, 30000], seed=8)
+    dev, out = [t.cuda() for t in host], [torch.empty_like(t.cuda()) for t in host]
+    norm, ws = torch.empty(1, device="cuda"), clip_workspace()
+    clip_grads(dev, 1.0, out=out, norm=norm, ws=ws)
+    torch.cuda.synchronize()
+    want, want_n = [t.clone() for t in out], norm.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            clip_grads(dev, 1.0, out=out, norm=norm, ws=ws)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(out, want)) and torch.equal(norm, want_n)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        clip_grads(dev, 1.0, out=out, norm=norm, ws=ws)
+    for t in dev:
+        t.mul_(2)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(norm, 2 * want_n)
+    for a, b in zip(out, want):   # the norm doubles, the factor halves (eps: 2^-27 of it)
+        assert bool(((a.double() - b.double()).abs() <= 2.0 ** -7 * b.double().abs()).all())
+
+
+def test_refusals():
+    a, b = torch.ones(8, device="cuda"), torch.ones(8, device="cuda")
+    with pytest.raises(XhcError, match="twice"):
+        clip_grads([a, b, a], 1.0)
+    with pytest.raises(XhcError, match="twice"):
+        clip_grads([a, b], 1.0, out=[a, a])
+    with pytest.raises(XhcError, match="like its gradient"):
+        clip_grads([a], 1.0, out=[b[:4]])
+    with pytest.raises(XhcError, match="fp32 or bf16"):
+        clip_grads([a.half()], 1.0)
+    with pytest.raises(XhcError, match="contiguous"):
+        clip_grads([torch.ones(4, 4, device="cuda").t()], 1.0)
+    with pytest.raises(XhcError, match="bytes"):
+        clip_grads([a], 1.0, ws=torch.empty(8, dtype=torch.uint8, device="cuda"))
+    for bad in (dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(max_norm=1.0, eps=-1.0), dict(max_norm=1.0, scale=INF)):
+        with pytest.raises(XhcError, match="invalid"):
+            clip_grads([a], **bad)
+    assert bool((a == 1).all())

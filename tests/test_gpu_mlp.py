@@ -1,0 +1,175 @@
+"""The gated feed-forward block against its 64-bit form: widths, token counts and activations at the edges of
+the tiles, every output inside guard bands, scratch and saved buffers poisoned before each call."""
+import pytest
+import torch
+
+import op_refs as R
+from paper_2607_14530_gb300 import synth
+from paper_2607_14530_gb300.xhc import Mlp, XhcError
+from xhc_cases import Guarded
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+NAMES = ("W_gate", "W_up", "W_down")
+
+
+def inputs(T, C, F, seed=0):
+    P = {"W_gate": synth.normal_bf16((F, C), seed + 1, C ** -0.5), "W_up": synth.normal_bf16((F, C), seed + 2, C ** -0.5),
+         "W_down": synth.normal_bf16((C, F), seed + 3, F ** -0.5)}
+    return synth.normal_bf16((T, C), seed + 4), {n: v.cuda() for n, v in P.items()}, synth.normal_bf16((T, C), seed + 5).cuda()
+
+
+def poisoned(op, T):
+    saved, ws = op.alloc_saved(T), op.alloc_workspace(T)
+    saved.fill_(0xFF)       # NaN as bf16 and as fp32
+    ws[256:].fill_(0xFF)
+    return saved, ws
+
+
+def run(op, x, P, dy, grad_dtype=BF, accumulate=False, start=None):
+    """{"y", "dx", the weight gradients} of one forward and backward, checked for stray writes."""
+    T = x.shape[0]
+    saved, ws = poisoned(op, T)
+    y, dx = Guarded(torch.full((T, op.C), float("nan"), dtype=BF)), Guarded(torch.full((T, op.C), float("nan"), dtype=BF))
+    first = lambda n, s: torch.full(s, float("nan"), dtype=grad_dtype) if start is None else start[n].to(grad_dtype)
+    grads = {n: Guarded(first(n, s)) for n, s in op.shapes().items()}
+    op.forward(P, x, ws, saved=saved, y=y.t)
+    op.backward(P, x, dy, {n: g.t for n, g in grads.items()}, saved, ws, dx=dx.t, accumulate=accumulate)
+    torch.cuda.synchronize()
+    assert int(ws[:4].view(torch.int32)) == 0
+    assert y.intact() and dx.intact() and all(g.intact() for g in grads.values())
+    return dict({n: g.t for n, g in grads.items()}, y=y.t, dx=dx.t)
+
+
+# token counts and widths on both sides of the tiles' 64, 128 and 256, the smallest of all, and odd multiples of 8
+SHAPES = [(1, 8, 8), (1, 264, 712), (2, 64, 128), (3, 72, 136), (7, 512, 1032), (16, 256, 520), (17, 1024, 2816), (31, 264, 712),
+          (32, 128, 64), (33, 128, 72), (64, 520, 1024), (65, 256, 384), (100, 2056, 264), (127, 512, 512), (128, 512, 512),
+          (129, 264, 712), (255, 384, 1000), (256, 1024, 256), (257, 256, 2048), (333, 264, 712), (700, 512, 1544),
+          (1029, 2048, 1384), (2500, 1024, 2816)]
+
+
+@pytest.mark.parametrize("T,C,F", SHAPES)
+def test_forward_and_backward(T, C, F):
+    act = ("silu", "gelu", "relu")[(T + C // 8 + F // 8) % 3]
+    x, P, dy = inputs(T, C, F, seed=T)
+    x = x.cuda()
+    got = run(Mlp(C, F, act), x, P, dy)
+    R.assert_mlp(got, R.mlp(x, P, act, dy))
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+@pytest.mark.parametrize("T", [1, 200, 1500])
+def test_activations_over_their_range(act, T):
+    """Gate values far out on both sides, where exponentials underflow and overflow."""
+    C, F = 128, 256
+    x, P, dy = inputs(T, C, F, seed=3)
+    P["W_gate"] *= torch.logspace(-2, 2, F, base=10.0, device="cuda")[:, None].to(BF)
+    got = run(Mlp(C, F, act), x.cuda(), P, dy)
+    R.assert_mlp(got, R.mlp(x.cuda(), P, act, dy))
+
+
+@pytest.mark.parametrize("T,C,F", [(1, 264, 712), (24, 512, 1544), (333, 264, 712), (1500, 512, 1024)])
+def test_inference_has_the_training_forwards_bits(T, C, F):
+    x, P, dy = inputs(T, C, F, seed=9)
+    x, op = x.cuda(), Mlp(C, F)
+    want = run(op, x, P, dy)["y"]
+    ws = poisoned(op, T)[1]
+    y = Guarded(torch.zeros(T, C, dtype=BF))
+    op.forward(P, x, ws, y=y.t)
+    torch.cuda.synchronize()
+    assert y.intact() and torch.equal(y.t, want)
+    assert torch.equal(op.forward(P, x, ws), want)
+
+
+@pytest.mark.parametrize("T,C,F", [(5, 72, 136), (333, 264, 712), (1029, 512, 1384)])
+def test_fp32_gradients_written_and_accumulated(T, C, F):
+    x, P, dy = inputs(T, C, F, seed=4)
+    x, op = x.cuda(), Mlp(C, F)
+    ref = R.mlp(x, P, "silu", dy)
+    got = run(op, x, P, dy, F32)
+    R.assert_mlp(got, ref, NAMES)
+    start = {n: torch.randn(s, generator=torch.Generator().manual_seed(1)) for n, s in op.shapes().items()}
+    more = run(op, x, P, dy, F32, True, start)
+    for n in NAMES:   # the same sums, added once in fp32
+        assert torch.equal(more[n], got[n] + start[n].cuda()), n
+    b = run(op, x, P, dy)
+    for n in NAMES:   # and rounded once
+        assert torch.equal(b[n], got[n].to(BF)), n
+
+
+def test_a_token_with_nan_stays_by_itself():
+    """Rows are independent: y and dx of the others keep their bits."""
+    for T in (24, 300):
+        x, P, dy = inputs(T, 256, 520, seed=6)
+        op = Mlp(256, 520)
+        want = run(op, x.cuda(), P, dy)
+        x[7, 3] = float("nan")
+        x[11, 0] = float("inf")
+        got = run(op, x.cuda(), P, dy)
+        keep = [t for t in range(T) if t not in (7, 11)]
+        for n in ("y", "dx"):
+            assert torch.equal(got[n][keep], want[n][keep])
+            assert bool(got[n][7].isnan().all()) and not bool(got[n][11].isfinite().all())
+
+
+@pytest.mark.parametrize("T,C,F", [(1, 512, 1032), (20, 512, 1032), (300, 264, 712), (1500, 512, 1024)])
+def test_streams_repeats_and_graphs(T, C, F):
+    """The same bits on another stream, again, and replayed from a captured graph with new inputs."""
+    x, P, dy = inputs(T, C, F, seed=8)
+    x, op = x.cuda(), Mlp(C, F)
+    want = run(op, x, P, dy)
+    saved, ws = poisoned(op, T)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    grads = {n: torch.empty_like(v) for n, v in P.items()}
+    side = torch.cuda.Stream()
+
+    def step():
+        op.forward(P, x, ws, saved=saved, y=y)
+        op.backward(P, x, dy, grads, saved, ws, dx=dx)
+
+    def same():
+        torch.cuda.synchronize()
+        return torch.equal(y, want["y"]) and torch.equal(dx, want["dx"]) and all(torch.equal(grads[n], want[n]) for n in NAMES)
+
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(20):
+            step()
+    assert same()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    old = x.clone()
+    x.copy_(old.flip(0))
+    graph.replay()
+    x.copy_(old)
+    torch.cuda.synchronize()
+    assert torch.equal(y.flip(0), want["y"])   # a token's result does not depend on its place
+    for t in (y, dx, *grads.values()):
+        t.fill_(float("nan"))
+    graph.replay()
+    assert same()
+
+
+def test_refusals():
+    x, P, dy = inputs(4, 64, 128)
+    x, op = x.cuda(), Mlp(64, 128)
+    saved, ws = op.alloc_saved(4), op.alloc_workspace(4)
+    grads = {n: torch.empty_like(v) for n, v in P.items()}
+    with pytest.raises(XhcError, match="x must be"):
+        op.forward(P, x.float(), ws)
+    with pytest.raises(XhcError, match="shape"):
+        op.forward(P, torch.zeros(4, 72, dtype=BF, device="cuda"), ws)
+    with pytest.raises(XhcError, match="contiguous"):
+        op.forward(P, torch.zeros(64, 4, dtype=BF, device="cuda").t(), ws)
+    with pytest.raises(XhcError, match="W_up"):
+        op.forward({n: v for n, v in P.items() if n != "W_up"}, x, ws)
+    with pytest.raises(XhcError, match="bytes"):
+        op.forward(P, torch.zeros(400, 64, dtype=BF, device="cuda"), ws)
+    with pytest.raises(XhcError, match="alignment"):
+        op.forward(P, torch.zeros(4 * 64 + 8, dtype=BF, device="cuda")[4:-4].view(4, 64), ws)
+    with pytest.raises(XhcError, match="accumulated"):
+        op.backward(P, x, dy, grads, saved, ws, accumulate=True)
+    with pytest.raises(XhcError, match="invalid"):
+        op.forward(P, x[:0], ws)

@@ -1,0 +1,93 @@
+"""The 64-bit forms that the operators are tested against: their gradients against differences, and the
+bounds on the kernels' roundings against the same roundings applied on the CPU."""
+import math
+
+import pytest
+import torch
+
+import op_refs as R
+
+F64 = torch.float64
+
+
+def _rand(*shape, seed, std=1.0):
+    return torch.randn(*shape, generator=torch.Generator().manual_seed(seed), dtype=F64) * std
+
+
+def _difference(f, t, idx, h=1e-5):
+    """Central difference of the scalar f in t[idx]: off by h^2 / 6 of the third derivative, and 2^-53 / h
+    of the value."""
+    old = float(t[idx])
+    t[idx] = old + h
+    a = float(f())
+    t[idx] = old - h
+    b = float(f())
+    t[idx] = old
+    return (a - b) / (2 * h)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_mlp_gradients_against_differences(act):
+    T, C, F = 5, 8, 16
+    x, dy = _rand(T, C, seed=1), _rand(T, C, seed=2)
+    P = {"W_gate": _rand(F, C, seed=3, std=C ** -0.5), "W_up": _rand(F, C, seed=4, std=C ** -0.5),
+         "W_down": _rand(C, F, seed=5, std=F ** -0.5)}
+    ref = R.mlp(x, P, act, dy)
+    loss = lambda: (R.mlp(x, P, act)["y"] * dy).sum()
+    for name, t in dict(P, dx=x).items():
+        for idx in ((0, 0), (2, 3), (4, 7)):
+            assert math.isclose(_difference(loss, t, idx), float(ref[name][idx]), rel_tol=1e-6, abs_tol=1e-7), (name, idx)
+
+
+def test_relu_gradients_against_differences():
+    """Away from its corner the block is a polynomial."""
+    T, C, F = 4, 8, 8
+    x, dy = _rand(T, C, seed=1), _rand(T, C, seed=2)
+    P = {"W_gate": _rand(F, C, seed=3), "W_up": _rand(F, C, seed=4), "W_down": _rand(C, F, seed=5)}
+    assert float((x @ P["W_gate"].T).abs().min()) > 1e-3
+    ref = R.mlp(x, P, "relu", dy)
+    loss = lambda: (R.mlp(x, P, "relu")["y"] * dy).sum()
+    for name, t in dict(P, dx=x).items():
+        assert math.isclose(_difference(loss, t, (1, 2)), float(ref[name][1, 2]), rel_tol=1e-6, abs_tol=1e-7), name
+
+
+@pytest.mark.parametrize("N", [1, 3])
+def test_norm_gradients_against_differences(N):
+    T, C, eps = 3, 8, 1e-5
+    X, w, dy = _rand(T, N, C, seed=1), 1 + 0.1 * _rand(C, seed=2), _rand(T, C, seed=3)
+    ref = R.sum_norm(X, w, eps, dy)
+    loss = lambda: (R.sum_norm(X, w, eps)["y"] * dy).sum()
+    for idx in ((0, 0, 0), (2, N - 1, 5)):
+        assert math.isclose(_difference(loss, X, idx), float(ref["dX"][idx]), rel_tol=1e-6, abs_tol=1e-7)
+    assert math.isclose(_difference(loss, w, (4,)), float(ref["dw"][4]), rel_tol=1e-6, abs_tol=1e-7)
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "relu"])
+def test_mlp_bounds_hold_for_the_documented_roundings(act):
+    T, C, F = 37, 64, 96
+    x, dy = _rand(T, C, seed=1).bfloat16(), _rand(T, C, seed=2).bfloat16()
+    P = {"W_gate": _rand(F, C, seed=3, std=C ** -0.5).bfloat16(), "W_up": _rand(F, C, seed=4, std=C ** -0.5).bfloat16(),
+         "W_down": _rand(C, F, seed=5, std=F ** -0.5).bfloat16()}
+    f = {n: v.float() for n, v in P.items()}
+    g, u = x.float() @ f["W_gate"].T, x.float() @ f["W_up"].T
+    q, dq = R.act(g, act)
+    bf = lambda v: v.bfloat16().float()
+    h, p, q = bf(q * u), bf(u * dq), bf(q)
+    dh = dy.float() @ f["W_down"]
+    dg, du = bf(dh * p), bf(dh * q)
+    got = {"y": h @ f["W_down"].T, "dx": dg @ f["W_gate"] + du @ f["W_up"], "W_gate": dg.T @ x.float(),
+           "W_up": du.T @ x.float(), "W_down": dy.float().T @ h}
+    ref = R.mlp(x, P, act, dy)
+    R.assert_mlp(got, ref)
+    R.assert_mlp({n: v.bfloat16() for n, v in got.items()}, ref)
+    # a mistake of the size of one weight's term is seen
+    got["W_down"][3, 5] *= 1.1
+    with pytest.raises(AssertionError):
+        R.assert_mlp({"W_down": got["W_down"]}, ref)
+
+
+def test_clip_form():
+    g = [torch.tensor([3.0, 0.0]), torch.tensor([[4.0]])]
+    norm, by, out = R.clip(g, 1.0, eps=0.0)
+    assert norm == 5.0 and by == 0.2 and float(out[1]) == 0.8
+    assert R.clip(g, 10.0, scale=0.5)[:2] == (2.5, 0.5)
