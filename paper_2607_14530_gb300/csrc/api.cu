@@ -1082,17 +1082,16 @@ namespace {
 
 // `saved` and `workspace` of the gated feed-forward block
 struct MlpLayout {
-    size_t h, p, q, saved_total;              // saved: bf16 [T][F], then p and q (mlp_pq_bytes each)
+    size_t h, pq, saved_total;                // saved: bf16 [T][F], then p and q (mlp_pq_bytes each)
     size_t err, hs, dg, du, ws_total;         // workspace: h of a forward without `saved` where dg is
 };
 
 MlpLayout mlp_layout(int64_t T, int F) {
     MlpLayout L;
-    const size_t tf = al((size_t)T * F * 2), pq = al(mlp_pq_bytes(T, F));
+    const size_t tf = al((size_t)T * F * 2);
     L.h = 0;
-    L.p = tf;
-    L.q = tf + pq;
-    L.saved_total = tf + 2 * pq;
+    L.pq = tf;
+    L.saved_total = al(tf + 2 * mlp_pq_bytes(T, F));
     L.err = 0;
     L.hs = L.dg = 256;
     L.du = L.dg + tf;
@@ -1148,8 +1147,8 @@ xhc_status xhc_mlp_fwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
     pdl.set((size_t)T * (C + F) * 2, st);
     uint16_t* h = (uint16_t*)(sv ? sv + L.h : ws + L.hs);
     int* err = (int*)(ws + L.err);
-    XHC_K("mlp_gate", st, launch_mlp_gate(T32, C, F, cfg->act, x, W->gate, W->up, h, sv ? sv + L.p : nullptr,
-                                          sv ? sv + L.q : nullptr, err, st));
+    XHC_K("mlp_gate", st, launch_mlp_gate(T32, C, F, cfg->act, x, W->gate, W->up, h,
+                                          sv ? sv + L.pq : nullptr, err, st));
     XHC_K("mlp_down", st, launch_mlp_down(T32, C, F, h, W->down, y, err, st));
     return XHC_OK;
 }
@@ -1176,10 +1175,10 @@ xhc_status xhc_mlp_bwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
     pdl.set((size_t)T * (C + F) * 2, st);
     uint16_t *dg = (uint16_t*)(ws + L.dg), *du = (uint16_t*)(ws + L.du);
     int* err = (int*)(ws + L.err);
-    XHC_K("mlp_dh", st, launch_mlp_dh(T32, C, F, dy, W->down, sv + L.p, sv + L.q, dg, du, err, st));
-    XHC_K("mlp_dx", st, launch_mlp_dx(T32, C, F, dg, du, W->gate, W->up, dx, err, st));
-    XHC_K("mlp_dw", st, launch_mlp_dw(T32, C, F, x, dy, (const uint16_t*)(sv + L.h), dg, du, g->gate, g->up, g->down,
-                                      grad_dtype == XHC_F32, accumulate, err, st));
+    const int f32 = grad_dtype == XHC_F32;
+    XHC_K("mlp_dh_dwd", st, launch_mlp_dh_dwd(T32, C, F, dy, W->down, (const uint16_t*)(sv + L.h), sv + L.pq, dg, du,
+                                              g->down, f32, accumulate, err, st));
+    XHC_K("mlp_dx_dw", st, launch_mlp_dx_dw(T32, C, F, x, dg, du, W->gate, W->up, dx, g->gate, g->up, f32, accumulate, err, st));
     return XHC_OK;
 }
 

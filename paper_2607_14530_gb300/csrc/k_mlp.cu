@@ -2,16 +2,20 @@
 //   forward   h = q u, q = act(g), g = x W_gate^T, u = x W_up^T;  y = h W_down^T
 //   backward  dh = dy W_down;  dg = dh p, p = u act'(g);  du = dh q
 //             dx = dg W_gate + du W_up;  dW_gate = dg^T x, dW_up = du^T x, dW_down = dy^T h
-// One persistent kernel template runs all of these products.  A tile of 128 CG x 128 CG outputs belongs to
-// a CTA (CG = 1) or to a pair of CTAs on two SMs (CG = 2: each stages half of A's rows and half of B's, the
-// MMA reads both halves, so an operand byte in shared memory feeds twice the products).  Operands arrive by
-// TMA in the memory's own order: K-major where a row holds the summed index, MN-major where it holds
-// the output's (the weights in the input gradients, both operands of the weight gradients), so nothing is
-// transposed.  Warp 0 loads, warp 1 issues the MMAs, warps 2..5 read the finished accumulator from TMEM
-// and store; two accumulators let the stores of a tile run under the products of the next.
-// Rounding: h, p, q, dg and du are stored as bf16 (once, from fp32): they are operands of the next product,
-// whose matrix instruction takes 16-bit operands; p and q rather than g and u, so that the
-// activation's derivative is formed from the fp32 g and the backward needs no activation at all.
+// One persistent kernel runs all of these products, several of them in a launch where none waits for another
+// (GemmProb: the backward takes dh with dW_down, then dx with dW_gate and dW_up).  A tile of 128 CG x
+// 128 CG outputs belongs to a CTA (CG = 1) or to a pair of CTAs on two SMs (CG = 2: each stages half of A's
+// rows and half of B's, the MMA reads both halves, so an operand byte in shared memory feeds twice the
+// products).  Operands arrive by TMA in the memory's own order: K-major where a row holds the summed index,
+// MN-major where it holds the output's (the weights in the input gradients, both operands of the weight
+// gradients), so nothing is transposed.  Warp 0 loads, warp 1 issues the MMAs, warps 2..9 read the finished
+// accumulator from TMEM, 32 rows and half of its columns each, and store through shared memory by TMA, which
+// also cuts off what a tile has past the output; two accumulators let that run under the next tile's products.
+// Rounding: h, dg and du are stored as bf16 (once, from fp32): they are operands of the next product, whose
+// matrix instruction takes 16-bit ones.  The backward forms dg and du from p and q rather than from g
+// and u: the derivative comes from the fp32 g, and no activation is evaluated again.  p and q keep the upper
+// 24 bits of fp32 (three bytes; 2^-16): as bf16 their rounding would come on top of that of dg
+// and du (dx off by 2.9e-3 of itself instead of 2.4e-3), and the bytes hide under the products.
 #include <math.h>
 
 #include "k_tc.cuh"
@@ -20,39 +24,87 @@ namespace xhc {
 
 namespace {
 
-constexpr int GM_NT = 192;
+constexpr int GM_EW = 8;                        // epilogue warps
+constexpr int GM_NT = 64 + 32 * GM_EW;
 constexpr int GM_BK = 64;                       // k-elements of a stage: one 128-byte swizzle row of bf16
 constexpr int GM_HALF = 128 * GM_BK * 2;        // one operand's bytes of a stage and CTA
 constexpr int GM_STAGE = 2 * GM_HALF;
 constexpr int GM_STAGES = 6;
-constexpr int GM_SMEM = GM_STAGES * GM_STAGE + (2 * GM_STAGES + 5) * 8 + 16 + 1024;
+constexpr int GM_STORE = 4096;                  // staging bytes of an epilogue warp: 32 rows of 128 bytes
+constexpr int GM_SMEM = GM_STAGES * GM_STAGE + GM_EW * GM_STORE + (2 * GM_STAGES + 5) * 8 + 16 + 1024;
 constexpr int GM_GROUP = 8;                     // tile rows walked together: their B tiles are shared in L2
 
-enum { EPI_GATE, EPI_OUT, EPI_DH };
-
-struct GemmMaps {
-    CUtensorMap a[3], b[3];
+// what becomes of an accumulator
+enum {
+    GM_GATE,    // gate and up columns side by side: h stored, p and q kept
+    GM_DH,      // dh: dg = dh p and du = dh q stored
+    GM_BF16,    // stored as bf16
+    GM_F32,     // stored as fp32
+    GM_ADD      // added to fp32
 };
 
+struct GemmMaps {
+    CUtensorMap a[4], b[4], o[3];
+};
+struct GemmProb {
+    int M, N;          // output rows and columns
+    int tm, tn;        // tiles
+    int first;         // its first tile
+    int kb1, kb;       // k-blocks of the first operand pair, and of both
+    int set, out;      // its first operand maps and output map
+    int kind, amn, bmn;
+};
 struct GemmArgs {
-    int nprob;              // problems (EPI_OUT: up to 3, each with its own operands; else 1)
-    int M[3], N[3];         // output rows and columns
-    int tm[3], tn[3];       // tiles
-    int first[4];           // first tile of each problem
-    int kb1, kb;            // k-blocks of the first operand pair and of both (EPI_OUT of one problem)
+    GemmProb p[3];
+    int nprob, tiles;
+    int na;                // tiles of the first problem: they are taken first
+    int head;              // rounds of other tiles taken by the CTAs with one tile fewer of these (gm_next)
     int act;
     uint64_t wait_ns;
     int* err;
-    void* out[3];           // EPI_GATE: h; EPI_OUT: the products; EPI_DH: dg, du
-    uint4* p;               // EPI_GATE (null: not kept), EPI_DH: p and q, see pq_at
-    uint4* q;
-    int f32, accumulate;    // EPI_OUT: fp32 outputs, added to what is there
+    unsigned char* pq;     // p, then q (null: not kept), see pq_at
+    int64_t q_off;
 };
 
-// p and q lie in blocks of 32 rows and 8 columns, a row's 16 bytes after the other: the 32 lanes of an
-// epilogue warp hold 32 rows of the same columns, and so write and read 512 contiguous bytes.
+// p and q lie in blocks of 32 rows and 8 columns, 24 bytes a row: the upper halves of a block's rows, 16 bytes
+// after 16 bytes, then the third bytes, 8 after 8.  The 32 lanes of an epilogue warp hold 32 rows of the same
+// columns and so write and read 512 and 256 contiguous bytes.
+constexpr int PQ_BLOCK = 32 * 24;
 __host__ __device__ __forceinline__ int64_t pq_at(int64_t row, int col, int F) {
-    return ((row >> 5) * (F / 8) + col / 8) * 32 + (row & 31);
+    return ((row >> 5) * (F / 8) + col / 8) * PQ_BLOCK;
+}
+// The upper 24 bits of 8 values (cut, not rounded: a carry could turn a NaN into another value)
+__device__ __forceinline__ void pq_store(unsigned char* blk, int lane, const float* v) {
+    uint32_t hi[4], lo[2];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) hi[e] = __byte_perm(__float_as_uint(v[2 * e]), __float_as_uint(v[2 * e + 1]), 0x7632);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint32_t a = __byte_perm(__float_as_uint(v[4 * e]), __float_as_uint(v[4 * e + 1]), 0x0051);
+        const uint32_t b = __byte_perm(__float_as_uint(v[4 * e + 2]), __float_as_uint(v[4 * e + 3]), 0x0051);
+        lo[e] = __byte_perm(a, b, 0x5410);
+    }
+    *reinterpret_cast<uint4*>(blk + lane * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint2*>(blk + 512 + lane * 8) = make_uint2(lo[0], lo[1]);
+}
+struct Pq8 {
+    uint4 hi;
+    uint2 lo;
+};
+__device__ __forceinline__ Pq8 pq_load(const unsigned char* blk, int lane) {
+    Pq8 r;
+    r.hi = ld_stream(blk + lane * 16);
+    asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(r.lo.x), "=r"(r.lo.y) : "l"(blk + 512 + lane * 8));
+    return r;
+}
+__device__ __forceinline__ void pq_unpack(const Pq8& r, float* v) {
+    const uint32_t hi[4] = {r.hi.x, r.hi.y, r.hi.z, r.hi.w}, lo[2] = {r.lo.x, r.lo.y};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        // bytes: 0, the low byte e of lo, the two of hi
+        const uint32_t l = __byte_perm(lo[e / 4], 0u, 0x4404u | ((uint32_t)(e & 3) << 4));
+        v[e] = __uint_as_float(__byte_perm(l, hi[e / 2], (e & 1) ? 0x7610 : 0x5410));
+    }
 }
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -110,16 +162,33 @@ __device__ __forceinline__ void gm_commit(uint32_t bar) {
     }
 }
 
-// act(g) and its derivative
+// 32 columns of a lane's row of TMEM; the wait is in the same statement
+__device__ __forceinline__ void tmem_ld32(uint32_t ta, float* v) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
+        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(ta));
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// act(g) and its derivative; exponentials and quotients in the fast forms (2^-21 or so), far below the
+// stored precision.  Where an exponential overflows the sigmoid is 0, as it should be.
 __device__ __forceinline__ void mlp_act(int act, float g, float& q, float& dq) {
     if (act == XHC_ACT_SILU) {
-        const float e = 1.0f / (1.0f + expf(-g));
-        q = g * e;
-        dq = e * (1.0f + g * (1.0f - e));
+        const float s = __fdividef(1.0f, 1.0f + __expf(-g));
+        q = g * s;
+        dq = s + q * (1.0f - s);
     } else if (act == XHC_ACT_GELU) {
         const float c = normcdff(g);
         q = g * c;
-        dq = c + g * 0.3989422804f * expf(-0.5f * g * g);
+        dq = c + g * 0.3989422804f * __expf(-0.5f * g * g);
     } else {
         q = g > 0.f ? g : g != g ? g : 0.f;
         dq = g > 0.f ? 1.f : 0.f;
@@ -132,23 +201,58 @@ struct GmTile {
 __device__ __forceinline__ GmTile gm_tile(const GemmArgs& a, int t) {
     GmTile r;
     r.p = 0;
-    while (r.p + 1 < a.nprob && t >= a.first[r.p + 1]) ++r.p;
-    t -= a.first[r.p];
-    const int per = GM_GROUP * a.tn[r.p], g = t / per, rows = min(GM_GROUP, a.tm[r.p] - g * GM_GROUP);
+    while (r.p + 1 < a.nprob && t >= a.p[r.p + 1].first) ++r.p;
+    const GemmProb& q = a.p[r.p];
+    t -= q.first;
+    const int per = GM_GROUP * q.tn, g = t / per, rows = min(GM_GROUP, q.tm - g * GM_GROUP);
     t -= g * per;
     r.n = t / rows;
     r.m = g * GM_GROUP + t - r.n * rows;
     return r;
 }
+// The tiles of cluster c of nc, one after the other (i = 0, 1, ...; -1: no more).  The first problem's, whose
+// tiles take longest, go round first; in the round that does not fill the GPU the clusters left out take
+// `head` rounds of the other problems' tiles, about as long as one of these; then all go on.
+__device__ __forceinline__ int gm_next(const GemmArgs& a, int c, int nc, int i) {
+    const int whole = a.na / nc, hi = a.na - whole * nc;   // clusters c < hi have one more
+    const int mine = whole + (c < hi ? 1 : 0);
+    if (i < mine) return c + i * nc;
+    i -= mine;
+    int t;
+    if (c >= hi && i < a.head) {
+        t = a.na + i * (nc - hi) + (c - hi);
+    } else {
+        if (c >= hi) i -= a.head;
+        t = a.na + a.head * (nc - hi) + i * nc + c;
+    }
+    return t < a.tiles ? t : -1;
+}
 
-template <int CG, bool AMN, bool BMN, int EPI>
-__global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ GemmMaps maps, GemmArgs a) {
-    constexpr int BM = 128 * CG, BN = 128 * CG;          // the tile
-    constexpr int TN = EPI == EPI_GATE ? BN / 2 : BN;    // output columns: gate and up share an accumulator
-    constexpr uint32_t COLS = 2 * BN;                    // TMEM columns: two accumulators
+// A warp's staged 32 rows go out; what lies past the output's edges is cut off.
+__device__ __forceinline__ void gm_store(const CUtensorMap* map, uint32_t src, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"((uint64_t)map),
+                 "r"(x), "r"(y), "r"(src)
+                 : "memory");
+}
+__device__ __forceinline__ void gm_store_add(const CUtensorMap* map, uint32_t src, int x, int y) {
+    asm volatile("cp.reduce.async.bulk.tensor.2d.global.shared::cta.add.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"((uint64_t)map),
+                 "r"(x), "r"(y), "r"(src)
+                 : "memory");
+}
+__device__ __forceinline__ void gm_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void gm_store_read_wait() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void gm_store_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void st_shared16(uint32_t a, uint4 v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+template <int CG>
+__global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmArgs a) {
+    constexpr int BM = 128 * CG, BN = 128 * CG;   // the tile
+    constexpr uint32_t COLS = 2 * BN;             // TMEM columns: two accumulators
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + GM_STAGES * GM_STAGE);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + GM_STAGES * GM_STAGE + GM_EW * GM_STORE);
     const uint32_t full = smem_u32(bars), empty = full + 8 * GM_STAGES, accfull = empty + 8 * GM_STAGES,
                    accempty = accfull + 16, drain = accempty + 16;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * GM_STAGES + 5);
@@ -156,7 +260,7 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
-    const int c0 = blockIdx.x / CG, nc = gridDim.x / CG, tiles = a.first[a.nprob];
+    const int c0 = blockIdx.x / CG, nc = gridDim.x / CG;
 
     if (threadIdx.x == 0) {
         s_abort = 0;
@@ -166,7 +270,7 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(accfull + 8 * s, 1);
-            mbar_init(accempty + 8 * s, 4 * CG);
+            mbar_init(accempty + 8 * s, GM_EW * CG);
         }
         mbar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -200,26 +304,27 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
             const uint32_t lead = CG == 2 ? map_rank(full, 0) : full;
             int s = 0, issued = 0;
             uint32_t ph = 0;
-            for (int t = c0; t < tiles && !aborted(); t += nc) {
+            for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
                 const GmTile tl = gm_tile(a, t);
-                const int m0 = tl.m * BM + (int)rank * 128, n0 = tl.n * TN;
-                for (int kb = 0; kb < a.kb; ++kb) {
+                const GemmProb& q = a.p[tl.p];
+                const int kind = q.kind, amn = q.amn, bmn = q.bmn, kb1 = q.kb1, kbs = q.kb, set0 = q.set;
+                const int m0 = tl.m * BM + (int)rank * 128, n0 = tl.n * (kind == GM_GATE ? BN / 2 : BN);
+                for (int kb = 0; kb < kbs; ++kb) {
                     if (issued >= GM_STAGES && !mbar_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
                         give_up(11);
                         break;
                     }
                     if (aborted()) break;
                     if (rank == 0) mbar_expect_tx(full + 8 * s, CG * GM_STAGE);
-                    const int set = EPI == EPI_OUT ? (a.nprob > 1 ? tl.p : kb >= a.kb1 ? 1 : 0) : 0;
-                    const int k0 = (set && a.nprob == 1 ? kb - a.kb1 : kb) * GM_BK;
+                    const int second = kb >= kb1 ? 1 : 0, set = set0 + second, k0 = (kb - (second ? kb1 : 0)) * GM_BK;
                     const uint32_t sa = smem_u32(smem + s * GM_STAGE), sb = sa + GM_HALF, bar = lead + 8 * s;
-                    if (AMN) {
+                    if (amn) {
                         gm_load<CG>(sa, &maps.a[set], m0, k0, bar);
                         gm_load<CG>(sa + GM_HALF / 2, &maps.a[set], m0 + 64, k0, bar);
                     } else {
                         gm_load<CG>(sa, &maps.a[set], k0, m0, bar);
                     }
-                    if (EPI == EPI_GATE) {
+                    if (kind == GM_GATE) {
                         // gate rows, then up rows: the halves of the accumulator's columns
                         if (CG == 2) {
                             gm_load<CG>(sb, &maps.b[rank], k0, n0, bar);
@@ -227,7 +332,7 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
                             gm_load<CG>(sb, &maps.b[0], k0, n0, bar);
                             gm_load<CG>(sb + GM_HALF / 2, &maps.b[1], k0, n0, bar);
                         }
-                    } else if (BMN) {
+                    } else if (bmn) {
                         gm_load<CG>(sb, &maps.b[set], n0 + (int)rank * 128, k0, bar);
                         gm_load<CG>(sb + GM_HALF / 2, &maps.b[set], n0 + (int)rank * 128 + 64, k0, bar);
                     } else {
@@ -257,30 +362,33 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
     } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
         if (lane == 0 && rank == 0) {
-            const uint32_t idesc = idesc_bf16(BM, BN, AMN) | ((BMN ? 1u : 0u) << 16);
-            int s = 0, i = 0;
+            int s = 0;
             uint32_t ph = 0;
-            for (int t = c0; t < tiles && !aborted(); t += nc, ++i) {
-                const int buf = i & 1;
+            for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
+                const GemmProb& q = a.p[gm_tile(a, t).p];
+                const bool amn = q.amn != 0, bmn = q.bmn != 0;
+                const int kbs = q.kb, buf = i & 1;
+                const uint32_t idesc = idesc_bf16(BM, BN, amn) | ((bmn ? 1u : 0u) << 16);
+                // 16 k-elements on.  K-major: 32 bytes in the swizzled row; MN-major: 16 rows of 128 bytes
+                const uint32_t da = (amn ? 2048u : 32u) >> 4, db = (bmn ? 2048u : 32u) >> 4;
                 if (i >= 2 && !mbar_wait(accempty + 8 * buf, (uint32_t)((i >> 1) & 1) ^ 1u, a.wait_ns)) {
                     give_up(12);
                     break;
                 }
                 tc_fence_after();
-                for (int kb = 0; kb < a.kb; ++kb) {
+                for (int kb = 0; kb < kbs; ++kb) {
                     if (!mbar_wait(full + 8 * s, ph, a.wait_ns)) {
                         give_up(13);
                         break;
                     }
                     tc_fence_after();
                     const uint32_t sa = smem_u32(smem + s * GM_STAGE), sb = sa + GM_HALF;
+                    const uint64_t A = amn ? sw128_desc_mn(sa, GM_HALF / 2) : sw128_desc(sa);
+                    const uint64_t B = bmn ? sw128_desc_mn(sb, GM_HALF / 2) : sw128_desc(sb);
 #pragma unroll
-                    for (int kk = 0; kk < GM_BK / 16; ++kk) {
-                        // K-major: 32 bytes on in the swizzled row; MN-major: 16 rows of 128 bytes on
-                        const uint64_t da = AMN ? sw128_desc_mn(sa + kk * 2048, GM_HALF / 2) : sw128_desc(sa + kk * 32);
-                        const uint64_t db = BMN ? sw128_desc_mn(sb + kk * 2048, GM_HALF / 2) : sw128_desc(sb + kk * 32);
-                        gm_mma<CG>(tmem + (uint32_t)(buf * BN), da, db, idesc, (kb | kk) ? 1u : 0u);
-                    }
+                    for (int kk = 0; kk < GM_BK / 16; ++kk)
+                        gm_mma<CG>(tmem + (uint32_t)(buf * BN), A + (uint64_t)(kk * da), B + (uint64_t)(kk * db), idesc,
+                                   (kb | kk) ? 1u : 0u);
                     gm_commit<CG>(empty + 8 * s);
                     if (++s == GM_STAGES) { s = 0; ph ^= 1u; }
                 }
@@ -293,91 +401,149 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
             }
         }
     } else {
-        // ---------------- epilogue (warps 2..5) ----------------
-        const int quarter = warp & 3;
+        // ---------------- epilogue (warps 2..9) ----------------
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
         const uint32_t free_bar = CG == 2 ? map_rank(accempty, 0) : accempty;
-        int i = 0;
-        for (int t = c0; t < tiles && !__any_sync(0xffffffffu, aborted()); t += nc, ++i) {
+        const uint32_t stage = smem_u32(smem + GM_STAGES * GM_STAGE + (warp - 2) * GM_STORE);
+        // the warp's staging memory can be written again / is written: its rows go out
+        auto stage_free = [&]() {
+            if (lane == 0) gm_store_read_wait();
+            __syncwarp();
+        };
+        auto stage_full = [&]() {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+        };
+        for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !__any_sync(0xffffffffu, aborted()); ++i) {
             const GmTile tl = gm_tile(a, t);
-            const int buf = i & 1;
+            const GemmProb& pr = a.p[tl.p];
+            const int kind = pr.kind, N = pr.N, out = pr.out, buf = i & 1;
+            const int tn = kind == GM_GATE ? BN / 2 : BN, w = tn / 2;          // the tile's and this warp's columns
+            const int row0 = tl.m * BM + (int)rank * 128 + quarter * 32, n0 = tl.n * tn + half * w;
+            const uint32_t acc = tmem + (uint32_t)(buf * BN + half * w) + ((uint32_t)(quarter * 32) << 16);
+            const int end = row0 < pr.M ? min(w, N - n0) : 0;                  // columns there are; may be negative
+            Pq8 pp[4], qq[4];
+            auto pq_fetch = [&](int c) {   // of 32 columns, before the accumulator is waited for
+#pragma unroll
+                for (int o = 0; o < 4; ++o)
+                    if (c + 8 * o < end) {
+                        const unsigned char* b = a.pq + pq_at(row0, n0 + c + 8 * o, N);
+                        pp[o] = pq_load(b, lane);
+                        qq[o] = pq_load(b + a.q_off, lane);
+                    }
+            };
+            if (kind == GM_DH) pq_fetch(0);
             if (!__all_sync(0xffffffffu, mbar_wait(accfull + 8 * buf, (uint32_t)((i >> 1) & 1), a.wait_ns))) {
                 if (lane == 0) give_up(14);
                 break;
             }
             tc_fence_after();
-            const int M = a.M[tl.p], N = a.N[tl.p];
-            const int row = tl.m * BM + (int)rank * 128 + quarter * 32 + lane, n0 = tl.n * TN;
-            const uint32_t acc = tmem + (uint32_t)(buf * BN) + ((uint32_t)(quarter * 32) << 16);
-            for (int c = 0; c < TN && n0 + c < N; c += 16) {
-                float v[16];
-                tmem_ld16(acc + c, v);
-                if (EPI == EPI_GATE) {
-                    float u[16], p[16];
-                    tmem_ld16(acc + TN + c, u);
+            auto release = [&]() {   // all of the accumulator that this warp reads is in registers
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if (CG == 2) mbar_arrive_cluster(free_bar + 8 * buf);
+                    else mbar_arrive(free_bar + 8 * buf);
+                }
+            };
+            if (end <= 0) {
+                release();
+                continue;
+            }
+            for (int c = 0; c < end; c += 32) {
+                const bool last = c + 32 >= end;
+                float v[32];
+                tmem_ld32(acc + c, v);
+                if (kind == GM_GATE) {
+                    float u[32];
+                    tmem_ld32(acc + tn + c, u);
+                    if (last) release();
+                    // 64 columns of h are staged, then stored (a single CTA's warps have 32)
+                    const int o0 = CG == 2 ? c & 32 : 0;
+                    if (o0 == 0) stage_free();
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float dq;
-                        mlp_act(a.act, v[e], v[e], dq);
-                        p[e] = u[e] * dq;
-                        u[e] *= v[e];
-                    }
-                    if (row < M) {
+                    for (int o = 0; o < 4; ++o) {
+                        float p[8], q[8], h[8];
 #pragma unroll
-                        for (int o = 0; o < 16; o += 8)
-                            if (n0 + c + o < N) {
-                                *reinterpret_cast<uint4*>((uint16_t*)a.out[0] + (int64_t)row * N + n0 + c + o) = pack8(u + o);
-                                if (a.p) {
-                                    a.p[pq_at(row, n0 + c + o, N)] = pack8(p + o);
-                                    a.q[pq_at(row, n0 + c + o, N)] = pack8(v + o);
-                                }
-                            }
-                    }
-                } else if (EPI == EPI_DH) {
-                    if (row < M) {
-#pragma unroll
-                        for (int o = 0; o < 16; o += 8)
-                            if (n0 + c + o < N) {
-                                float p[8], q[8];
-                                unpack8(a.p[pq_at(row, n0 + c + o, N)], p);
-                                unpack8(a.q[pq_at(row, n0 + c + o, N)], q);
-#pragma unroll
-                                for (int e = 0; e < 8; ++e) {
-                                    p[e] *= v[o + e];
-                                    q[e] *= v[o + e];
-                                }
-                                const int64_t at = (int64_t)row * N + n0 + c + o;
-                                *reinterpret_cast<uint4*>((uint16_t*)a.out[0] + at) = pack8(p);
-                                *reinterpret_cast<uint4*>((uint16_t*)a.out[1] + at) = pack8(q);
-                            }
-                    }
-                } else if (row < M) {
-#pragma unroll
-                    for (int o = 0; o < 16; o += 8)
-                        if (n0 + c + o < N) {
-                            const int64_t at = (int64_t)row * N + n0 + c + o;
-                            if (!a.f32) {
-                                *reinterpret_cast<uint4*>((uint16_t*)a.out[tl.p] + at) = pack8(v + o);
-                            } else {
-                                float4* to = reinterpret_cast<float4*>((float*)a.out[tl.p] + at);
-                                float4 x = make_float4(v[o], v[o + 1], v[o + 2], v[o + 3]), z = make_float4(v[o + 4], v[o + 5], v[o + 6], v[o + 7]);
-                                if (a.accumulate) {
-                                    const float4 x0 = to[0], z0 = to[1];
-                                    x.x += x0.x; x.y += x0.y; x.z += x0.z; x.w += x0.w;
-                                    z.x += z0.x; z.y += z0.y; z.z += z0.z; z.w += z0.w;
-                                }
-                                to[0] = x;
-                                to[1] = z;
-                            }
+                        for (int e = 0; e < 8; ++e) {
+                            float dq;
+                            mlp_act(a.act, v[8 * o + e], q[e], dq);
+                            p[e] = u[8 * o + e] * dq;
+                            h[e] = u[8 * o + e] * q[e];
                         }
+                        st_shared16(stage + (CG == 2 ? lane * 128 + (((o0 / 8 + o) ^ (lane & 7)) << 4)
+                                                     : lane * 64 + ((o ^ ((lane >> 1) & 3)) << 4)),
+                                    pack8(h));
+                        if (a.pq && c + 8 * o < end) {
+                            unsigned char* b = a.pq + pq_at(row0, n0 + c + 8 * o, N);
+                            pq_store(b, lane, p);
+                            pq_store(b + a.q_off, lane, q);
+                        }
+                    }
+                    if (o0 || last) {
+                        stage_full();
+                        if (lane == 0) {
+                            gm_store(&maps.o[out], stage, n0 + c - o0, row0);
+                            gm_store_commit();
+                        }
+                    }
+                } else if (kind == GM_DH) {
+                    if (last) release();
+                    stage_free();
+#pragma unroll
+                    for (int o = 0; o < 4; ++o) {
+                        float p[8], q[8];
+                        pq_unpack(pp[o], p);
+                        pq_unpack(qq[o], q);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            p[e] *= v[8 * o + e];
+                            q[e] *= v[8 * o + e];
+                        }
+                        const uint32_t at = stage + lane * 64 + ((o ^ ((lane >> 1) & 3)) << 4);
+                        st_shared16(at, pack8(p));
+                        st_shared16(at + 2048, pack8(q));
+                    }
+                    if (!last) pq_fetch(c + 32);
+                    stage_full();
+                    if (lane == 0) {
+                        gm_store(&maps.o[out], stage, n0 + c, row0);
+                        gm_store(&maps.o[out + 1], stage + 2048, n0 + c, row0);
+                        gm_store_commit();
+                    }
+                } else if (kind == GM_BF16) {
+                    if (last) release();
+                    const int o0 = c & 32;
+                    if (o0 == 0) stage_free();
+#pragma unroll
+                    for (int o = 0; o < 4; ++o)
+                        st_shared16(stage + lane * 128 + (((o0 / 8 + o) ^ (lane & 7)) << 4), pack8(v + 8 * o));
+                    if (o0 || last) {
+                        stage_full();
+                        if (lane == 0) {
+                            gm_store(&maps.o[out], stage, n0 + c - o0, row0);
+                            gm_store_commit();
+                        }
+                    }
+                } else {
+                    if (last) release();
+                    stage_free();
+#pragma unroll
+                    for (int o = 0; o < 8; ++o)
+                        st_shared16(stage + lane * 128 + ((o ^ (lane & 7)) << 4),
+                                    make_uint4(__float_as_uint(v[4 * o]), __float_as_uint(v[4 * o + 1]),
+                                               __float_as_uint(v[4 * o + 2]), __float_as_uint(v[4 * o + 3])));
+                    stage_full();
+                    if (lane == 0) {
+                        if (kind == GM_ADD) gm_store_add(&maps.o[out], stage, n0 + c, row0);
+                        else gm_store(&maps.o[out], stage, n0 + c, row0);
+                        gm_store_commit();
+                    }
                 }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if (CG == 2) mbar_arrive_cluster(free_bar + 8 * buf);
-                else mbar_arrive(free_bar + 8 * buf);
-            }
         }
+        if (lane == 0) gm_store_wait();
+        __syncwarp();
     }
     tc_fence_before();
     __syncthreads();
@@ -391,15 +557,70 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
 
 // ---- host ----
 
-// A launch of CG-CTA clusters: as many as the GPU holds at once, at most one per tile.  (An SM without a
-// partner in its cluster of SMs takes no pair: the driver says how many fit.)
-template <int CG, bool AMN, bool BMN, int EPI>
-cudaError_t gm_launch(const GemmMaps& maps, const GemmArgs& a, cudaStream_t st) {
-    auto* k = k_mlp_gemm<CG, AMN, BMN, EPI>;
-    cudaError_t e = smem_optin((const void*)k, GM_SMEM);
-    if (e != cudaSuccess) return e;
+// Clusters of CG CTAs that the GPU holds at once.  (An SM without a partner in its group of SMs takes no pair:
+// the driver says how many fit.)
+template <int CG>
+cudaError_t gm_clusters(int* most) {
+    *most = device_sms();
+    cudaError_t e = smem_optin((const void*)k_mlp_gemm<CG>, GM_SMEM);
+    if (e != cudaSuccess || CG == 1) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(GM_NT);
+    cfg.gridDim = dim3(device_sms() / 2 * 2);
+    cfg.dynamicSmemBytes = GM_SMEM;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = CG;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(most, k_mlp_gemm<CG>, &cfg);
+    return e == cudaSuccess && *most < 1 ? cudaErrorInvalidConfiguration : e;
+}
+
+// Tiles of all problems, and the order of gm_next
+void gm_tiles(GemmArgs& a, int cg, int clusters) {
+    a.tiles = 0;
+    for (int p = 0; p < a.nprob; ++p) {
+        GemmProb& q = a.p[p];
+        const int bm = 128 * cg, tn = q.kind == GM_GATE ? bm / 2 : bm;
+        q.tm = (q.M + bm - 1) / bm;
+        q.tn = (q.N + tn - 1) / tn;
+        q.first = a.tiles;
+        a.tiles += q.tm * q.tn;
+    }
+    a.na = a.p[0].tm * a.p[0].tn;
+    a.head = 0;
+    const int nc = a.tiles < clusters ? a.tiles : clusters, left = nc - a.na % nc;
+    if (a.nprob > 1 && left < nc) {
+        // k-blocks, and about 8 for a tile's own start and end
+        a.head = (a.p[0].kb + 8) / (a.p[1].kb + 8);
+        const int most = (a.tiles - a.na) / left;
+        if (a.head > most) a.head = most;
+    }
+}
+
+// k-blocks, in those of one 128 x 128 tile, that the busiest cluster walks
+int64_t gm_cost(GemmArgs& a, int cg, int clusters) {
+    gm_tiles(a, cg, clusters);
+    int64_t work = 0, most = 0;
+    for (int p = 0; p < a.nprob; ++p) {
+        const int64_t k = a.p[p].kb + 8;
+        work += k * a.p[p].tm * a.p[p].tn;
+        most = k > most ? k : most;
+    }
+    const int nc = a.tiles < clusters ? a.tiles : clusters;
+    // one kind of tile: whole rounds; several: they fill each other's gaps but for half of one
+    const int64_t rounds = a.nprob == 1 ? most * ((a.tiles + nc - 1) / nc) : work / nc + most / 2;
+    return rounds < most ? most : rounds;
+}
+
+template <int CG>
+cudaError_t gm_launch(const GemmMaps& maps, GemmArgs& a, int clusters, cudaStream_t st) {
+    gm_tiles(a, CG, clusters);
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(GM_NT);
+    cfg.gridDim = dim3(CG * (a.tiles < clusters ? a.tiles : clusters));
     cfg.dynamicSmemBytes = GM_SMEM;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
@@ -409,59 +630,47 @@ cudaError_t gm_launch(const GemmMaps& maps, const GemmArgs& a, cudaStream_t st) 
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
-    cfg.numAttrs = 1;
-    int most = device_sms();
-    if (CG == 2) {
-        cfg.gridDim = dim3(device_sms() / 2 * 2);
-        if ((e = cudaOccupancyMaxActiveClusters(&most, k, &cfg)) != cudaSuccess) return e;
-        if (most < 1) return cudaErrorInvalidConfiguration;
-    }
-    const int tiles = a.first[a.nprob];
-    cfg.gridDim = dim3(CG * (tiles < most ? tiles : most));
     cfg.numAttrs = pdl_on() ? 2 : 1;
-    e = cudaLaunchKernelEx(&cfg, k, maps, a);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_mlp_gemm<CG>, maps, a);
     note_launch();
     return e == cudaSuccess ? cudaGetLastError() : e;
 }
 
-// Pairs or single CTAs: the time of a product's last wave counts.  A single CTA's tile has a quarter of a
-// pair's products on half the SMs and reads twice the shared memory for them.
-bool gm_pairs(int64_t tiles2, int64_t tiles1) {
-    const int sms = device_sms();
-    const int64_t w2 = (tiles2 + sms / 2 - 1) / (sms / 2), w1 = (tiles1 + sms - 1) / sms;
-    return 10 * 2 * w2 <= 13 * w1;
+// Pairs or single CTAs, by the busiest cluster's k-blocks: a pair's tile has four times a single CTA's
+// products on twice the tensor cores, in 1.6 times as long (a single CTA reads its operands from
+// shared memory as fast as that allows).
+struct GmPlan {
+    int cg, clusters;
+};
+cudaError_t gm_plan(GemmArgs& a, GmPlan* pl) {
+    int n1 = 0, n2 = 0;
+    cudaError_t e = gm_clusters<1>(&n1);
+    if (e == cudaSuccess) e = gm_clusters<2>(&n2);
+    if (e != cudaSuccess) return e;
+    const int64_t c1 = gm_cost(a, 1, n1), c2 = gm_cost(a, 2, n2);
+    pl->cg = 16 * c2 <= 10 * c1 ? 2 : 1;
+    pl->clusters = pl->cg == 2 ? n2 : n1;
+    return cudaSuccess;
+}
+cudaError_t gm_run(const GemmMaps& maps, GemmArgs& a, const GmPlan& pl, cudaStream_t st) {
+    return pl.cg == 2 ? gm_launch<2>(maps, a, pl.clusters, st) : gm_launch<1>(maps, a, pl.clusters, st);
 }
 
-void gm_tiles(GemmArgs& a, int cg, bool gate) {
-    a.first[0] = 0;
-    for (int p = 0; p < a.nprob; ++p) {
-        const int bm = 128 * cg, tn = gate ? bm / 2 : bm;
-        a.tm[p] = (a.M[p] + bm - 1) / bm;
-        a.tn[p] = (a.N[p] + tn - 1) / tn;
-        a.first[p + 1] = a.first[p] + a.tm[p] * a.tn[p];
-    }
+GemmProb gm_prob(int M, int N, int K, int kind, int amn, int bmn, int set, int out) {
+    GemmProb p = {};
+    p.M = M;
+    p.N = N;
+    p.kb1 = p.kb = (K + GM_BK - 1) / GM_BK;
+    p.kind = kind;
+    p.amn = amn;
+    p.bmn = bmn;
+    p.set = set;
+    p.out = out;
+    return p;
 }
-
-template <bool AMN, bool BMN, int EPI>
-cudaError_t gm_run(const GemmMaps& maps, GemmArgs& a, int cg, cudaStream_t st) {
-    gm_tiles(a, cg, EPI == EPI_GATE);
-    if (cg == 2) return gm_launch<2, AMN, BMN, EPI>(maps, a, st);
-    return gm_launch<1, AMN, BMN, EPI>(maps, a, st);
-}
-
-int gm_choose(GemmArgs& a, bool gate) {
-    gm_tiles(a, 2, gate);
-    const int t2 = a.first[a.nprob];
-    gm_tiles(a, 1, gate);
-    return gm_pairs(t2, a.first[a.nprob]) ? 2 : 1;
-}
-
-GemmArgs gm_args(int M, int N, int K, int* err) {
+GemmArgs gm_args(int nprob, int* err) {
     GemmArgs a = {};
-    a.nprob = 1;
-    a.M[0] = M;
-    a.N[0] = N;
-    a.kb1 = a.kb = (K + GM_BK - 1) / GM_BK;
+    a.nprob = nprob;
     a.err = err;
     a.wait_ns = debug_wait_ns();
     return a;
@@ -475,90 +684,96 @@ bool map_k(CUtensorMap* m, const void* p, int rows, int inner, int box) {
 bool map_mn(CUtensorMap* m, const void* p, int k, int outs) {
     return make_map_box(m, p, (uint64_t)outs, (uint64_t)k, 64, GM_BK);
 }
+// output [rows][cols] of bf16 or fp32, stored 32 rows and `bytes` (64 or 128) of them at a time
+bool map_out(CUtensorMap* m, const void* p, int rows, int cols, bool f32, int bytes) {
+    auto enc = get_encode();
+    if (!enc) return false;
+    const int es = f32 ? 4 : 2;
+    cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
+    cuuint64_t gstride[1] = {(cuuint64_t)cols * es};
+    cuuint32_t box[2] = {(cuuint32_t)(bytes / es), 32};
+    cuuint32_t one[2] = {1, 1};
+    return enc(m, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(p), gdim,
+               gstride, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 }  // namespace
 
-size_t mlp_pq_bytes(int64_t T, int F) { return (size_t)((T + 31) / 32 * 32) * F * 2; }
+size_t mlp_pq_bytes(int64_t T, int F) { return (size_t)((T + 31) / 32) * (F / 8) * PQ_BLOCK; }
 
 cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, const uint16_t* Wg, const uint16_t* Wu,
-                            uint16_t* h, void* p, void* q, int* err, cudaStream_t st) {
-    GemmArgs a = gm_args(T, F, C, err);
+                            uint16_t* h, void* pq, int* err, cudaStream_t st) {
+    GemmArgs a = gm_args(1, err);
+    a.p[0] = gm_prob(T, F, C, GM_GATE, 0, 0, 0, 0);
     a.act = act;
-    a.out[0] = h;
-    a.p = (uint4*)p;
-    a.q = (uint4*)q;
-    const int cg = gm_choose(a, true);
-    GemmMaps m;
-    if (!map_k(&m.a[0], x, T, C, 128) || !map_k(&m.b[0], Wg, F, C, 64 * cg) || !map_k(&m.b[1], Wu, F, C, 64 * cg))
+    a.pq = (unsigned char*)pq;
+    a.q_off = (int64_t)mlp_pq_bytes(T, F);
+    GmPlan pl;
+    const cudaError_t e = gm_plan(a, &pl);
+    if (e != cudaSuccess) return e;
+    GemmMaps m = {};
+    if (!map_k(&m.a[0], x, T, C, 128) || !map_k(&m.b[0], Wg, F, C, 64 * pl.cg) || !map_k(&m.b[1], Wu, F, C, 64 * pl.cg) ||
+        !map_out(&m.o[0], h, T, F, false, 64 * pl.cg))
         return cudaErrorInvalidValue;
-    m.a[1] = m.a[2] = m.a[0];
-    m.b[2] = m.b[0];
-    return gm_run<false, false, EPI_GATE>(m, a, cg, st);
+    return gm_run(m, a, pl, st);
 }
 
 cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, int* err,
                             cudaStream_t st) {
-    GemmArgs a = gm_args(T, C, F, err);
-    a.out[0] = y;
-    const int cg = gm_choose(a, false);
-    GemmMaps m;
-    if (!map_k(&m.a[0], h, T, F, 128) || !map_k(&m.b[0], Wd, C, F, 128)) return cudaErrorInvalidValue;
-    m.a[1] = m.a[2] = m.a[0];
-    m.b[1] = m.b[2] = m.b[0];
-    return gm_run<false, false, EPI_OUT>(m, a, cg, st);
+    GemmArgs a = gm_args(1, err);
+    a.p[0] = gm_prob(T, C, F, GM_BF16, 0, 0, 0, 0);
+    GmPlan pl;
+    const cudaError_t e = gm_plan(a, &pl);
+    if (e != cudaSuccess) return e;
+    GemmMaps m = {};
+    if (!map_k(&m.a[0], h, T, F, 128) || !map_k(&m.b[0], Wd, C, F, 128) || !map_out(&m.o[0], y, T, C, false, 128))
+        return cudaErrorInvalidValue;
+    return gm_run(m, a, pl, st);
 }
 
-cudaError_t launch_mlp_dh(int T, int C, int F, const uint16_t* dy, const uint16_t* Wd, const void* p, const void* q,
-                          uint16_t* dg, uint16_t* du, int* err, cudaStream_t st) {
-    GemmArgs a = gm_args(T, F, C, err);
-    a.p = (uint4*)const_cast<void*>(p);
-    a.q = (uint4*)const_cast<void*>(q);
-    a.out[0] = dg;
-    a.out[1] = du;
-    const int cg = gm_choose(a, false);
-    GemmMaps m;
-    if (!map_k(&m.a[0], dy, T, C, 128) || !map_mn(&m.b[0], Wd, C, F)) return cudaErrorInvalidValue;
-    m.a[1] = m.a[2] = m.a[0];
-    m.b[1] = m.b[2] = m.b[0];
-    return gm_run<false, true, EPI_DH>(m, a, cg, st);
+cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uint16_t* Wd, const uint16_t* h, const void* pq,
+                              uint16_t* dg, uint16_t* du, void* dWd, int f32, int accumulate, int* err, cudaStream_t st) {
+    GemmArgs a = gm_args(2, err);
+    const GemmProb dh = gm_prob(T, F, C, GM_DH, 0, 1, 0, 0);
+    const GemmProb dw = gm_prob(C, F, T, !f32 ? GM_BF16 : accumulate ? GM_ADD : GM_F32, 1, 1, 1, 2);
+    a.p[0] = dh.kb >= dw.kb ? dh : dw;   // the longer tiles first
+    a.p[1] = dh.kb >= dw.kb ? dw : dh;
+    a.pq = (unsigned char*)const_cast<void*>(pq);
+    a.q_off = (int64_t)mlp_pq_bytes(T, F);
+    GmPlan pl;
+    const cudaError_t e = gm_plan(a, &pl);
+    if (e != cudaSuccess) return e;
+    GemmMaps m = {};
+    if (!map_k(&m.a[0], dy, T, C, 128) || !map_mn(&m.b[0], Wd, C, F) || !map_mn(&m.a[1], dy, T, C) || !map_mn(&m.b[1], h, T, F) ||
+        !map_out(&m.o[0], dg, T, F, false, 64) || !map_out(&m.o[1], du, T, F, false, 64) ||
+        !map_out(&m.o[2], dWd, C, F, f32 != 0, 128))
+        return cudaErrorInvalidValue;
+    return gm_run(m, a, pl, st);
 }
 
-cudaError_t launch_mlp_dx(int T, int C, int F, const uint16_t* dg, const uint16_t* du, const uint16_t* Wg,
-                          const uint16_t* Wu, uint16_t* dx, int* err, cudaStream_t st) {
-    GemmArgs a = gm_args(T, C, F, err);
-    a.kb = 2 * a.kb1;
-    a.out[0] = dx;
-    const int cg = gm_choose(a, false);
-    GemmMaps m;
+cudaError_t launch_mlp_dx_dw(int T, int C, int F, const uint16_t* x, const uint16_t* dg, const uint16_t* du,
+                             const uint16_t* Wg, const uint16_t* Wu, uint16_t* dx, void* dWg, void* dWu, int f32,
+                             int accumulate, int* err, cudaStream_t st) {
+    GemmArgs a = gm_args(3, err);
+    const int kind = !f32 ? GM_BF16 : accumulate ? GM_ADD : GM_F32;
+    GemmProb d = gm_prob(T, C, F, GM_BF16, 0, 1, 0, 0);
+    d.kb = 2 * d.kb1;
+    a.p[0] = d;
+    a.p[1] = gm_prob(F, C, T, kind, 1, 1, 2, 1);
+    a.p[2] = gm_prob(F, C, T, kind, 1, 1, 3, 2);
+    GmPlan pl;
+    const cudaError_t e = gm_plan(a, &pl);
+    if (e != cudaSuccess) return e;
+    GemmMaps m = {};
     if (!map_k(&m.a[0], dg, T, F, 128) || !map_k(&m.a[1], du, T, F, 128) || !map_mn(&m.b[0], Wg, F, C) ||
-        !map_mn(&m.b[1], Wu, F, C))
+        !map_mn(&m.b[1], Wu, F, C) || !map_mn(&m.a[2], dg, T, F) || !map_mn(&m.a[3], du, T, F) || !map_mn(&m.b[2], x, T, C) ||
+        !map_out(&m.o[0], dx, T, C, false, 128) || !map_out(&m.o[1], dWg, F, C, f32 != 0, 128) ||
+        !map_out(&m.o[2], dWu, F, C, f32 != 0, 128))
         return cudaErrorInvalidValue;
-    m.a[2] = m.a[0];
-    m.b[2] = m.b[0];
-    return gm_run<false, true, EPI_OUT>(m, a, cg, st);
-}
-
-cudaError_t launch_mlp_dw(int T, int C, int F, const uint16_t* x, const uint16_t* dy, const uint16_t* h,
-                          const uint16_t* dg, const uint16_t* du, void* dWg, void* dWu, void* dWd, int f32,
-                          int accumulate, int* err, cudaStream_t st) {
-    GemmArgs a = gm_args(F, C, T, err);
-    a.nprob = 3;
-    a.M[1] = F;
-    a.N[1] = C;
-    a.M[2] = C;
-    a.N[2] = F;
-    a.out[0] = dWg;
-    a.out[1] = dWu;
-    a.out[2] = dWd;
-    a.f32 = f32;
-    a.accumulate = accumulate;
-    const int cg = gm_choose(a, false);
-    GemmMaps m;
-    if (!map_mn(&m.a[0], dg, T, F) || !map_mn(&m.a[1], du, T, F) || !map_mn(&m.a[2], dy, T, C) ||
-        !map_mn(&m.b[0], x, T, C) || !map_mn(&m.b[2], h, T, F))
-        return cudaErrorInvalidValue;
-    m.b[1] = m.b[0];
-    return gm_run<true, true, EPI_OUT>(m, a, cg, st);
+    m.b[3] = m.b[2];
+    return gm_run(m, a, pl, st);
 }
 
 }  // namespace xhc

@@ -737,17 +737,17 @@ cudaError_t launch_clip(const ClipTensors& t, double scale, double max_norm, dou
 
 // bytes of p (and of q) of the gated feed-forward block
 size_t mlp_pq_bytes(int64_t T, int F);
-// h = q u, p = u act'(g), q = act(g); p null: only h
+// h = q u; pq: p = u act'(g), then q = act(g) (null: only h)
 cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, const uint16_t* Wg, const uint16_t* Wu,
-                            uint16_t* h, void* p, void* q, int* err, cudaStream_t st);
+                            uint16_t* h, void* pq, int* err, cudaStream_t st);
 cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, int* err,
                             cudaStream_t st);
-cudaError_t launch_mlp_dh(int T, int C, int F, const uint16_t* dy, const uint16_t* Wd, const void* p, const void* q,
-                          uint16_t* dg, uint16_t* du, int* err, cudaStream_t st);
-cudaError_t launch_mlp_dx(int T, int C, int F, const uint16_t* dg, const uint16_t* du, const uint16_t* Wg,
-                          const uint16_t* Wu, uint16_t* dx, int* err, cudaStream_t st);
-cudaError_t launch_mlp_dw(int T, int C, int F, const uint16_t* x, const uint16_t* dy, const uint16_t* h,
-                          const uint16_t* dg, const uint16_t* du, void* dWg, void* dWu, void* dWd, int f32,
-                          int accumulate, int* err, cudaStream_t st);
+// dg = dh p and du = dh q of dh = dy W_down, and dW_down = dy^T h (f32: fp32, accumulate: added)
+cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uint16_t* Wd, const uint16_t* h, const void* pq,
+                              uint16_t* dg, uint16_t* du, void* dWd, int f32, int accumulate, int* err, cudaStream_t st);
+// dx = dg W_gate + du W_up, dW_gate = dg^T x, dW_up = du^T x
+cudaError_t launch_mlp_dx_dw(int T, int C, int F, const uint16_t* x, const uint16_t* dg, const uint16_t* du,
+                             const uint16_t* Wg, const uint16_t* Wu, uint16_t* dx, void* dWg, void* dWu, int f32,
+                             int accumulate, int* err, cudaStream_t st);
 
 }  // namespace xhc
