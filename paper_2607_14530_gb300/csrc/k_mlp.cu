@@ -3,20 +3,27 @@
 //   backward  dh = dy W_down;  dg = dh p, p = u act'(g);  du = dh q
 //             dx = dg W_gate + du W_up;  dW_gate = dg^T x, dW_up = du^T x, dW_down = dy^T h
 // One persistent kernel runs all of these products, several of them in a launch where none waits for another
-// (GemmProb: the backward takes dh with dW_down, then dx with dW_gate and dW_up).  A tile of 128 CG x
-// 128 CG outputs belongs to a CTA (CG = 1) or to a pair of CTAs on two SMs (CG = 2: each stages half of A's
-// rows and half of B's, the MMA reads both halves, so an operand byte in shared memory feeds twice the
-// products).  Operands arrive by TMA in the memory's own order: K-major where a row holds the summed index,
+// (GemmProb: the backward takes dh with dW_down, then dx with dW_gate and dW_up).  A pair of CTAs on two SMs
+// takes 256 x BN outputs: each stages half of A's rows and half of B's, the MMA (cta_group::2) reads both
+// halves.  What bounds large products then is how fast the SMs are fed from L2: 32 KB an SM for each
+// 64 k-elements at BN = 256, 64 bytes a clock at the tensor cores' full rate, where about 50 arrive
+// (measured: a stage of 64 k-elements took 650 clocks instead of 512, and 490 instead of 256 with a
+// single CTA's 128 x 128 tile).  So two pairs form a cluster and share what they have in common, each CTA
+// loading half of it for both by TMA multicast (GmShape).
+// Operands arrive in the memory's own order: K-major where a row holds the summed index,
 // MN-major where it holds the output's (the weights in the input gradients, both operands of the weight
-// gradients), so nothing is transposed.  Warp 0 loads, warp 1 issues the MMAs, warps 2..9 read the finished
-// accumulator from TMEM, 32 rows and half of its columns each, and store through shared memory by TMA, which
-// also cuts off what a tile has past the output; two accumulators let that run under the next tile's products.
+// gradients), so nothing is transposed; every box is 64 x 64 elements (8 KB).  Warp 0 loads, warp 1 issues the MMAs, warps 2..9 read the
+// finished accumulator from TMEM, 32 rows and half of its columns each, and store through shared memory by
+// TMA, which also cuts off what a tile has past the output; two accumulators let that run under the next
+// tile's products.
 // Rounding: h, dg and du are stored as bf16 (once, from fp32): they are operands of the next product, whose
 // matrix instruction takes 16-bit ones.  The backward forms dg and du from p and q rather than from g
 // and u: the derivative comes from the fp32 g, and no activation is evaluated again.  p and q keep the upper
 // 24 bits of fp32 (three bytes; 2^-16): as bf16 their rounding would come on top of that of dg
 // and du (dx off by 2.9e-3 of itself instead of 2.4e-3), and the bytes hide under the products.
 #include <math.h>
+
+#include <type_traits>
 
 #include "k_tc.cuh"
 
@@ -27,12 +34,25 @@ namespace {
 constexpr int GM_EW = 8;                        // epilogue warps
 constexpr int GM_NT = 64 + 32 * GM_EW;
 constexpr int GM_BK = 64;                       // k-elements of a stage: one 128-byte swizzle row of bf16
-constexpr int GM_HALF = 128 * GM_BK * 2;        // one operand's bytes of a stage and CTA
-constexpr int GM_STAGE = 2 * GM_HALF;
-constexpr int GM_STAGES = 6;
+constexpr int GM_BOX = 64 * GM_BK * 2;          // bytes of a TMA box
 constexpr int GM_STORE = 4096;                  // staging bytes of an epilogue warp: 32 rows of 128 bytes
-constexpr int GM_SMEM = GM_STAGES * GM_STAGE + GM_EW * GM_STORE + (2 * GM_STAGES + 5) * 8 + 16 + 1024;
-constexpr int GM_GROUP = 8;                     // tile rows walked together: their B tiles are shared in L2
+
+// A cluster: PM x PN pairs of CTAs, 256 x BN outputs each.
+//   <2, 1, 256>  B shared: 24 KB an SM for 512 clocks of products
+//   <1, 1, 256>  nothing shared: 32 KB for 512 clocks; the GPU holds 152 SMs' worth of pairs, but 144 of fours
+//   <1, 2, 128>  A shared: 16 KB for 256 clocks; half of the first one's outputs a cluster, for smaller products
+template <int PM_, int PN_, int BN_>
+struct GmShape {
+    static constexpr int PM = PM_, PN = PN_, BN = BN_;
+    static constexpr int PAIRS = PM * PN, CTAS = 2 * PAIRS;
+    static constexpr int A_BYTES = 2 * GM_BOX, B_BYTES = BN / 128 * GM_BOX, STAGE = A_BYTES + B_BYTES;
+    static constexpr int STAGES = BN == 256 ? 6 : 8;
+    static constexpr int SMEM = STAGES * STAGE + GM_EW * GM_STORE + (2 * STAGES + 5) * 8 + 16 + 1024;
+    static constexpr int GROUP = 8 / PM;   // tile rows walked together: their B tiles are shared in L2
+};
+
+// Clocks that a tile costs beside its products, as far as they do not run under another's
+constexpr int GM_TILE_CLOCKS = 4000;
 
 // what becomes of an accumulator
 enum {
@@ -51,6 +71,7 @@ struct GemmProb {
     int tm, tn;        // tiles
     int first;         // its first tile
     int kb1, kb;       // k-blocks of the first operand pair, and of both
+    int group;         // tile rows walked together
     int set, out;      // its first operand maps and output map
     int kind, amn, bmn;
 };
@@ -125,41 +146,32 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t a) {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(a) : "memory");
 }
 
-template <int CG>
+// a box into this CTA's shared memory, or into that of every CTA of `mask` (at the same place); the barrier at
+// `bar` is the even CTA's of the pair, with a mask that of every such CTA's pair
 __device__ __forceinline__ void gm_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    if (CG == 1) {
-        tma_load_2d(dst, map, x, y, bar);
-    } else {
-        // own shared memory, the barrier of the pair's first CTA
-        asm volatile(
-            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
-            " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"((uint64_t)map), "r"(x), "r"(y), "r"(bar)
-            : "memory");
-    }
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"((uint64_t)map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
 }
-template <int CG>
+__device__ __forceinline__ void gm_load_mc(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar, uint16_t mask) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster"
+        " [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(dst), "l"((uint64_t)map), "r"(x), "r"(y), "r"(bar), "h"(mask)
+        : "memory");
+}
 __device__ __forceinline__ void gm_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accum) {
-    if (CG == 1) {
-        mma_bf16(d, a, b, idesc, accum);
-    } else {
-        asm volatile(
-            "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-            " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
-            "r"(accum)
-            : "memory");
-    }
+    asm volatile(
+        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+        " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc),
+        "r"(accum)
+        : "memory");
 }
-// the barrier at this offset, in both CTAs of a pair, is arrived at when the MMAs issued so far are done
-template <int CG>
-__device__ __forceinline__ void gm_commit(uint32_t bar) {
-    if (CG == 1) {
-        mma_commit(bar);
-    } else {
-        asm volatile(
-            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
-            "h"((uint16_t)3)
-            : "memory");
-    }
+// the barrier at this offset, in every CTA of `mask`, is arrived at when the pair's MMAs issued so far are done
+__device__ __forceinline__ void gm_commit(uint32_t bar, uint16_t mask) {
+    asm volatile(
+        "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(mask)
+        : "memory");
 }
 
 // 32 columns of a lane's row of TMEM; the wait is in the same statement
@@ -178,20 +190,27 @@ __device__ __forceinline__ void tmem_ld32(uint32_t ta, float* v) {
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
-// act(g) and its derivative; exponentials and quotients in the fast forms (2^-21 or so), far below the
-// stored precision.  Where an exponential overflows the sigmoid is 0, as it should be.
-__device__ __forceinline__ void mlp_act(int act, float g, float& q, float& dq) {
-    if (act == XHC_ACT_SILU) {
-        const float s = __fdividef(1.0f, 1.0f + __expf(-g));
-        q = g * s;
-        dq = s + q * (1.0f - s);
-    } else if (act == XHC_ACT_GELU) {
-        const float c = normcdff(g);
-        q = g * c;
-        dq = c + g * 0.3989422804f * __expf(-0.5f * g * g);
-    } else {
-        q = g > 0.f ? g : g != g ? g : 0.f;
-        dq = g > 0.f ? 1.f : 0.f;
+// q = act(g), p = u act'(g) and h = q u of 8 columns; exponentials and quotients in the fast forms (2^-21 or
+// so), far below the stored precision.  Where an exponential overflows the sigmoid is 0, as it should be.
+template <int ACT>
+__device__ __forceinline__ void mlp_act8(const float* g, const float* u, float* p, float* q, float* h) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float dq;
+        if (ACT == XHC_ACT_SILU) {
+            const float s = __fdividef(1.0f, 1.0f + __expf(-g[e]));
+            q[e] = g[e] * s;
+            dq = s + q[e] * (1.0f - s);
+        } else if (ACT == XHC_ACT_GELU) {
+            const float c = normcdff(g[e]);
+            q[e] = g[e] * c;
+            dq = c + g[e] * 0.3989422804f * __expf(-0.5f * g[e] * g[e]);
+        } else {
+            q[e] = g[e] > 0.f ? g[e] : g[e] != g[e] ? g[e] : 0.f;
+            dq = g[e] > 0.f ? 1.f : 0.f;
+        }
+        p[e] = u[e] * dq;
+        h[e] = u[e] * q[e];
     }
 }
 
@@ -204,10 +223,10 @@ __device__ __forceinline__ GmTile gm_tile(const GemmArgs& a, int t) {
     while (r.p + 1 < a.nprob && t >= a.p[r.p + 1].first) ++r.p;
     const GemmProb& q = a.p[r.p];
     t -= q.first;
-    const int per = GM_GROUP * q.tn, g = t / per, rows = min(GM_GROUP, q.tm - g * GM_GROUP);
+    const int per = q.group * q.tn, g = t / per, rows = min(q.group, q.tm - g * q.group);
     t -= g * per;
     r.n = t / rows;
-    r.m = g * GM_GROUP + t - r.n * rows;
+    r.m = g * q.group + t - r.n * rows;
     return r;
 }
 // The tiles of cluster c of nc, one after the other (i = 0, 1, ...; -1: no more).  The first problem's, whose
@@ -246,48 +265,45 @@ __device__ __forceinline__ void st_shared16(uint32_t a, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(a), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
-template <int CG>
+template <class S>
 __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ GemmMaps maps, const __grid_constant__ GemmArgs a) {
-    constexpr int BM = 128 * CG, BN = 128 * CG;   // the tile
+    constexpr int BN = S::BN, STAGES = S::STAGES;
     constexpr uint32_t COLS = 2 * BN;             // TMEM columns: two accumulators
+    constexpr uint16_t ALL = (1u << S::CTAS) - 1;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + GM_STAGES * GM_STAGE + GM_EW * GM_STORE);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * GM_STAGES, accfull = empty + 8 * GM_STAGES,
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + STAGES * S::STAGE + GM_EW * GM_STORE);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, accfull = empty + 8 * STAGES,
                    accempty = accfull + 16, drain = accempty + 16;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * GM_STAGES + 5);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 5);
     __shared__ int s_abort;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = CG == 2 ? cluster_rank() : 0u;
-    const int c0 = blockIdx.x / CG, nc = gridDim.x / CG;
+    const int rank = (int)cluster_rank(), half = rank & 1, pair = rank >> 1;   // half of the pair's operands and rows
+    const int pm = S::PM > 1 ? pair : 0, pn = S::PN > 1 ? pair : 0;
+    const int c0 = blockIdx.x / S::CTAS, nc = gridDim.x / S::CTAS;
 
     if (threadIdx.x == 0) {
         s_abort = 0;
-        for (int s = 0; s < GM_STAGES; ++s) {
-            mbar_init(full + 8 * s, 1);
-            mbar_init(empty + 8 * s, 1);
+        for (int s = 0; s < STAGES; ++s) {
+            mbar_init(full + 8 * s, 1);            // the even CTA's: both CTAs' operands are there
+            mbar_init(empty + 8 * s, S::PAIRS);    // every pair's MMAs have read them
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(accfull + 8 * s, 1);
-            mbar_init(accempty + 8 * s, GM_EW * CG);
+            mbar_init(accempty + 8 * s, GM_EW * 2);
         }
         mbar_init(drain, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 1) {
-        if (CG == 1) {
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(COLS) : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-        } else {
-            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(COLS) : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-        }
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(COLS) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
-    if (CG == 2) cluster_sync();
+    cluster_sync();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     pdl_entry();
@@ -301,74 +317,76 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
     if (warp == 0) {
         // ---------------- TMA producer ----------------
         if (lane == 0) {
-            const uint32_t lead = CG == 2 ? map_rank(full, 0) : full;
+            const uint32_t lead = map_rank(full, (uint32_t)(rank & ~1));
+            const uint16_t mates = (uint16_t)(0x5u << half);   // this half's CTAs of both pairs
             int s = 0, issued = 0;
             uint32_t ph = 0;
             for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
                 const GmTile tl = gm_tile(a, t);
                 const GemmProb& q = a.p[tl.p];
-                const int kind = q.kind, amn = q.amn, bmn = q.bmn, kb1 = q.kb1, kbs = q.kb, set0 = q.set;
-                const int m0 = tl.m * BM + (int)rank * 128, n0 = tl.n * (kind == GM_GATE ? BN / 2 : BN);
+                const int gate = q.kind == GM_GATE, amn = q.amn, bmn = q.bmn, kb1 = q.kb1, kbs = q.kb, set0 = q.set;
+                const int m0 = (tl.m * S::PM + pm) * 256 + half * 128;
+                // gate rows in the even CTA, up rows in the odd one: the halves of the accumulator's columns
+                const int n0 = gate ? (tl.n * S::PN + pn) * (BN / 2) : (tl.n * S::PN + pn) * BN + half * (BN / 2);
                 for (int kb = 0; kb < kbs; ++kb) {
-                    if (issued >= GM_STAGES && !mbar_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
+                    if (issued >= STAGES && !mbar_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
                         give_up(11);
                         break;
                     }
                     if (aborted()) break;
-                    if (rank == 0) mbar_expect_tx(full + 8 * s, CG * GM_STAGE);
+                    if (half == 0) mbar_expect_tx(full + 8 * s, 2 * S::STAGE);
                     const int second = kb >= kb1 ? 1 : 0, set = set0 + second, k0 = (kb - (second ? kb1 : 0)) * GM_BK;
-                    const uint32_t sa = smem_u32(smem + s * GM_STAGE), sb = sa + GM_HALF, bar = lead + 8 * s;
-                    if (amn) {
-                        gm_load<CG>(sa, &maps.a[set], m0, k0, bar);
-                        gm_load<CG>(sa + GM_HALF / 2, &maps.a[set], m0 + 64, k0, bar);
+                    const uint32_t sa = smem_u32(smem + s * S::STAGE), sb = sa + S::A_BYTES, bar = lead + 8 * s;
+                    const CUtensorMap *ma = &maps.a[set], *mb = &maps.b[gate ? half : set];
+                    // a box's place along the operand's 64-row blocks
+                    auto load = [&](uint32_t dst, const CUtensorMap* m, int mn, int at, int blk, bool shared) {
+                        const int x = mn ? at + 64 * blk : k0, y = mn ? k0 : at + 64 * blk;
+                        if (shared) gm_load_mc(dst + blk * GM_BOX, m, x, y, bar, mates);
+                        else gm_load(dst + blk * GM_BOX, m, x, y, bar);
+                    };
+                    if (S::PN > 1) {
+                        load(sa, ma, amn, m0, pair, true);
                     } else {
-                        gm_load<CG>(sa, &maps.a[set], k0, m0, bar);
+                        load(sa, ma, amn, m0, 0, false);
+                        load(sa, ma, amn, m0, 1, false);
                     }
-                    if (kind == GM_GATE) {
-                        // gate rows, then up rows: the halves of the accumulator's columns
-                        if (CG == 2) {
-                            gm_load<CG>(sb, &maps.b[rank], k0, n0, bar);
-                        } else {
-                            gm_load<CG>(sb, &maps.b[0], k0, n0, bar);
-                            gm_load<CG>(sb + GM_HALF / 2, &maps.b[1], k0, n0, bar);
-                        }
-                    } else if (bmn) {
-                        gm_load<CG>(sb, &maps.b[set], n0 + (int)rank * 128, k0, bar);
-                        gm_load<CG>(sb + GM_HALF / 2, &maps.b[set], n0 + (int)rank * 128 + 64, k0, bar);
+                    if (S::PM > 1) {
+                        load(sb, mb, bmn, n0, pair, true);
                     } else {
-                        gm_load<CG>(sb, &maps.b[set], k0, n0 + (int)rank * 128, bar);
+                        load(sb, mb, bmn, n0, 0, false);
+                        if (BN == 256) load(sb, mb, bmn, n0, 1, false);
                     }
                     ++issued;
-                    if (++s == GM_STAGES) { s = 0; ph ^= 1u; }
+                    if (++s == STAGES) { s = 0; ph ^= 1u; }
                 }
             }
             if (!aborted()) {
-                // the MMAs' releases of the last stages reach both CTAs of a pair before either ends
-                for (int q = 0; q < GM_STAGES; ++q) {
-                    if (issued + q >= GM_STAGES && !mbar_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
+                // the MMAs' releases of the last stages reach every CTA of the cluster before one ends
+                for (int q = 0; q < STAGES; ++q) {
+                    if (issued + q >= STAGES && !mbar_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
                         give_up(15);
                         break;
                     }
-                    if (++s == GM_STAGES) { s = 0; ph ^= 1u; }
+                    if (++s == STAGES) { s = 0; ph ^= 1u; }
                 }
-            } else if (rank == 0) {
+            } else if (half == 0) {
                 // a wait ran out: the copies in flight land before this memory is given back
-                for (int q = 0; q < GM_STAGES && q < issued; ++q) {
-                    if (--s < 0) { s = GM_STAGES - 1; ph ^= 1u; }
+                for (int q = 0; q < STAGES && q < issued; ++q) {
+                    if (--s < 0) { s = STAGES - 1; ph ^= 1u; }
                     mbar_wait(full + 8 * s, ph, a.wait_ns);
                 }
             }
         }
     } else if (warp == 1) {
-        // ---------------- MMA issuer ----------------
-        if (lane == 0 && rank == 0) {
+        // ---------------- MMA issuer (the even CTA of a pair) ----------------
+        if (lane == 0 && half == 0) {
             int s = 0;
             uint32_t ph = 0;
             for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
                 const GemmProb& q = a.p[gm_tile(a, t).p];
                 const bool amn = q.amn != 0, bmn = q.bmn != 0;
                 const int kbs = q.kb, buf = i & 1;
-                const uint32_t idesc = idesc_bf16(BM, BN, amn) | ((bmn ? 1u : 0u) << 16);
+                const uint32_t idesc = idesc_bf16(256, BN, amn) | ((bmn ? 1u : 0u) << 16);
                 // 16 k-elements on.  K-major: 32 bytes in the swizzled row; MN-major: 16 rows of 128 bytes
                 const uint32_t da = (amn ? 2048u : 32u) >> 4, db = (bmn ? 2048u : 32u) >> 4;
                 if (i >= 2 && !mbar_wait(accempty + 8 * buf, (uint32_t)((i >> 1) & 1) ^ 1u, a.wait_ns)) {
@@ -382,29 +400,29 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t sa = smem_u32(smem + s * GM_STAGE), sb = sa + GM_HALF;
-                    const uint64_t A = amn ? sw128_desc_mn(sa, GM_HALF / 2) : sw128_desc(sa);
-                    const uint64_t B = bmn ? sw128_desc_mn(sb, GM_HALF / 2) : sw128_desc(sb);
+                    const uint32_t sa = smem_u32(smem + s * S::STAGE), sb = sa + S::A_BYTES;
+                    const uint64_t A = amn ? sw128_desc_mn(sa, GM_BOX) : sw128_desc(sa);
+                    const uint64_t B = bmn ? sw128_desc_mn(sb, GM_BOX) : sw128_desc(sb);
 #pragma unroll
                     for (int kk = 0; kk < GM_BK / 16; ++kk)
-                        gm_mma<CG>(tmem + (uint32_t)(buf * BN), A + (uint64_t)(kk * da), B + (uint64_t)(kk * db), idesc,
-                                   (kb | kk) ? 1u : 0u);
-                    gm_commit<CG>(empty + 8 * s);
-                    if (++s == GM_STAGES) { s = 0; ph ^= 1u; }
+                        gm_mma(tmem + (uint32_t)(buf * BN), A + (uint64_t)(kk * da), B + (uint64_t)(kk * db), idesc,
+                               (kb | kk) ? 1u : 0u);
+                    gm_commit(empty + 8 * s, ALL);
+                    if (++s == STAGES) { s = 0; ph ^= 1u; }
                 }
                 if (aborted()) break;
-                gm_commit<CG>(accfull + 8 * buf);
+                gm_commit(accfull + 8 * buf, (uint16_t)(3u << (2 * pair)));
             }
             if (aborted()) {   // the MMAs issued so far end before TMEM is given back
-                gm_commit<CG>(drain);
+                gm_commit(drain, (uint16_t)(1u << rank));
                 mbar_wait(drain, 0, a.wait_ns);
             }
         }
     } else {
         // ---------------- epilogue (warps 2..9) ----------------
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
-        const uint32_t free_bar = CG == 2 ? map_rank(accempty, 0) : accempty;
-        const uint32_t stage = smem_u32(smem + GM_STAGES * GM_STAGE + (warp - 2) * GM_STORE);
+        const int quarter = warp & 3, side = (warp - 2) >> 2;
+        const uint32_t free_bar = map_rank(accempty, (uint32_t)(rank & ~1));
+        const uint32_t stage = smem_u32(smem + STAGES * S::STAGE + (warp - 2) * GM_STORE);
         // the warp's staging memory can be written again / is written: its rows go out
         auto stage_free = [&]() {
             if (lane == 0) gm_store_read_wait();
@@ -419,8 +437,8 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
             const GemmProb& pr = a.p[tl.p];
             const int kind = pr.kind, N = pr.N, out = pr.out, buf = i & 1;
             const int tn = kind == GM_GATE ? BN / 2 : BN, w = tn / 2;          // the tile's and this warp's columns
-            const int row0 = tl.m * BM + (int)rank * 128 + quarter * 32, n0 = tl.n * tn + half * w;
-            const uint32_t acc = tmem + (uint32_t)(buf * BN + half * w) + ((uint32_t)(quarter * 32) << 16);
+            const int row0 = (tl.m * S::PM + pm) * 256 + half * 128 + quarter * 32, n0 = (tl.n * S::PN + pn) * tn + side * w;
+            const uint32_t acc = tmem + (uint32_t)(buf * BN + side * w) + ((uint32_t)(quarter * 32) << 16);
             const int end = row0 < pr.M ? min(w, N - n0) : 0;                  // columns there are; may be negative
             Pq8 pp[4], qq[4];
             auto pq_fetch = [&](int c) {   // of 32 columns, before the accumulator is waited for
@@ -441,10 +459,7 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
             auto release = [&]() {   // all of the accumulator that this warp reads is in registers
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) {
-                    if (CG == 2) mbar_arrive_cluster(free_bar + 8 * buf);
-                    else mbar_arrive(free_bar + 8 * buf);
-                }
+                if (lane == 0) mbar_arrive_cluster(free_bar + 8 * buf);
             };
             if (end <= 0) {
                 release();
@@ -458,28 +473,27 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
                     float u[32];
                     tmem_ld32(acc + tn + c, u);
                     if (last) release();
-                    // 64 columns of h are staged, then stored (a single CTA's warps have 32)
-                    const int o0 = CG == 2 ? c & 32 : 0;
+                    // 64 columns of h are staged, then stored (a warp has 32 at BN = 128)
+                    const int o0 = BN == 256 ? c & 32 : 0;
                     if (o0 == 0) stage_free();
+                    auto columns = [&](auto act) {
 #pragma unroll
-                    for (int o = 0; o < 4; ++o) {
-                        float p[8], q[8], h[8];
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            float dq;
-                            mlp_act(a.act, v[8 * o + e], q[e], dq);
-                            p[e] = u[8 * o + e] * dq;
-                            h[e] = u[8 * o + e] * q[e];
+                        for (int o = 0; o < 4; ++o) {
+                            float p[8], q[8], h[8];
+                            mlp_act8<decltype(act)::value>(v + 8 * o, u + 8 * o, p, q, h);
+                            st_shared16(stage + (BN == 256 ? lane * 128 + (((o0 / 8 + o) ^ (lane & 7)) << 4)
+                                                           : lane * 64 + ((o ^ ((lane >> 1) & 3)) << 4)),
+                                        pack8(h));
+                            if (a.pq && c + 8 * o < end) {
+                                unsigned char* b = a.pq + pq_at(row0, n0 + c + 8 * o, N);
+                                pq_store(b, lane, p);
+                                pq_store(b + a.q_off, lane, q);
+                            }
                         }
-                        st_shared16(stage + (CG == 2 ? lane * 128 + (((o0 / 8 + o) ^ (lane & 7)) << 4)
-                                                     : lane * 64 + ((o ^ ((lane >> 1) & 3)) << 4)),
-                                    pack8(h));
-                        if (a.pq && c + 8 * o < end) {
-                            unsigned char* b = a.pq + pq_at(row0, n0 + c + 8 * o, N);
-                            pq_store(b, lane, p);
-                            pq_store(b + a.q_off, lane, q);
-                        }
-                    }
+                    };
+                    if (a.act == XHC_ACT_SILU) columns(std::integral_constant<int, XHC_ACT_SILU>{});
+                    else if (a.act == XHC_ACT_GELU) columns(std::integral_constant<int, XHC_ACT_GELU>{});
+                    else columns(std::integral_constant<int, XHC_ACT_RELU>{});
                     if (o0 || last) {
                         stage_full();
                         if (lane == 0) {
@@ -547,45 +561,29 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
     }
     tc_fence_before();
     __syncthreads();
-    if (CG == 2) cluster_sync();   // the pair's MMAs, arrivals and copies are done in both CTAs
+    cluster_sync();   // the cluster's MMAs, arrivals and copies are done in every CTA
     if (warp == 1) {
         tc_fence_after();
-        if (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS) : "memory");
-        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS) : "memory");
     }
 }
 
 // ---- host ----
 
-// Clusters of CG CTAs that the GPU holds at once.  (An SM without a partner in its group of SMs takes no pair:
-// the driver says how many fit.)
-template <int CG>
-cudaError_t gm_clusters(int* most) {
-    *most = device_sms();
-    cudaError_t e = smem_optin((const void*)k_mlp_gemm<CG>, GM_SMEM);
-    if (e != cudaSuccess || CG == 1) return e;
-    cudaLaunchConfig_t cfg = {};
-    cfg.blockDim = dim3(GM_NT);
-    cfg.gridDim = dim3(device_sms() / 2 * 2);
-    cfg.dynamicSmemBytes = GM_SMEM;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = CG;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    cfg.attrs = at;
-    cfg.numAttrs = 1;
-    e = cudaOccupancyMaxActiveClusters(most, k_mlp_gemm<CG>, &cfg);
-    return e == cudaSuccess && *most < 1 ? cudaErrorInvalidConfiguration : e;
-}
+using GmTall = GmShape<2, 1, 256>;
+using GmPair = GmShape<1, 1, 256>;
+using GmWide = GmShape<1, 2, 128>;
 
 // Tiles of all problems, and the order of gm_next
-void gm_tiles(GemmArgs& a, int cg, int clusters) {
+template <class S>
+void gm_tiles(GemmArgs& a, int clusters) {
     a.tiles = 0;
     for (int p = 0; p < a.nprob; ++p) {
         GemmProb& q = a.p[p];
-        const int bm = 128 * cg, tn = q.kind == GM_GATE ? bm / 2 : bm;
+        const int bm = 256 * S::PM, tn = (q.kind == GM_GATE ? S::BN / 2 : S::BN) * S::PN;
         q.tm = (q.M + bm - 1) / bm;
         q.tn = (q.N + tn - 1) / tn;
+        q.group = S::GROUP;
         q.first = a.tiles;
         a.tiles += q.tm * q.tn;
     }
@@ -600,60 +598,83 @@ void gm_tiles(GemmArgs& a, int cg, int clusters) {
     }
 }
 
-// k-blocks, in those of one 128 x 128 tile, that the busiest cluster walks
-int64_t gm_cost(GemmArgs& a, int cg, int clusters) {
-    gm_tiles(a, cg, clusters);
-    int64_t work = 0, most = 0;
-    for (int p = 0; p < a.nprob; ++p) {
-        const int64_t k = a.p[p].kb + 8;
-        work += k * a.p[p].tm * a.p[p].tn;
-        most = k > most ? k : most;
-    }
-    const int nc = a.tiles < clusters ? a.tiles : clusters;
-    // one kind of tile: whole rounds; several: they fill each other's gaps but for half of one
-    const int64_t rounds = a.nprob == 1 ? most * ((a.tiles + nc - 1) / nc) : work / nc + most / 2;
-    return rounds < most ? most : rounds;
-}
-
-template <int CG>
-cudaError_t gm_launch(const GemmMaps& maps, GemmArgs& a, int clusters, cudaStream_t st) {
-    gm_tiles(a, CG, clusters);
+template <class S>
+cudaLaunchConfig_t gm_config(cudaLaunchAttribute* at, int clusters) {
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(GM_NT);
-    cfg.gridDim = dim3(CG * (a.tiles < clusters ? a.tiles : clusters));
-    cfg.dynamicSmemBytes = GM_SMEM;
-    cfg.stream = st;
-    cudaLaunchAttribute at[2];
+    cfg.gridDim = dim3(S::CTAS * clusters);
+    cfg.dynamicSmemBytes = S::SMEM;
     at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = CG;
+    at[0].val.clusterDim.x = S::CTAS;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cfg;
+}
+
+// One way to run a launch, and its time in clocks as far as tiles tell it
+struct GmPlan {
+    int shape, clusters;
+    int64_t clocks;
+};
+
+// Clusters that the GPU holds at once (an SM without partners in its group of SMs takes none: the driver says how
+// many fit, 76 pairs or 36 fours of 152 SMs), and the busiest one's clocks: `per` for a stage of 64
+// k-elements and GM_TILE_CLOCKS for a tile.
+template <class S>
+cudaError_t gm_try(GemmArgs& a, int shape, int per, GmPlan* best) {
+    const void* k = (const void*)k_mlp_gemm<S>;
+    cudaError_t e = smem_optin(k, S::SMEM);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute at[2];
+    const cudaLaunchConfig_t cfg = gm_config<S>(at, device_sms() / S::CTAS);
+    int n = 0;
+    e = cudaOccupancyMaxActiveClusters(&n, k_mlp_gemm<S>, &cfg);
+    if (e != cudaSuccess) return e;
+    if (n < 1) return cudaSuccess;
+    gm_tiles<S>(a, n);
+    const int nc = a.tiles < n ? a.tiles : n;
+    // the first problem's tiles go round, then the rest (gm_next)
+    const int64_t ta = (int64_t)a.p[0].kb * per + GM_TILE_CLOCKS, tb = a.nprob > 1 ? (int64_t)a.p[1].kb * per + GM_TILE_CLOCKS : 0;
+    const int whole = a.na / nc, hi = a.na % nc, rest = a.tiles - a.na - a.head * (nc - hi), r = rest / nc, one = rest % nc;
+    const int64_t lo = whole * ta + (a.head + r + (one > hi ? 1 : 0)) * tb;
+    const int64_t up = hi ? (whole + 1) * ta + (r + (one ? 1 : 0)) * tb : 0;
+    const int64_t clocks = lo > up ? lo : up;
+    if (best->clocks < 0 || clocks < best->clocks) {
+        best->shape = shape;
+        best->clusters = n;
+        best->clocks = clocks;
+    }
+    return cudaSuccess;
+}
+
+cudaError_t gm_plan(GemmArgs& a, GmPlan* pl) {
+    *pl = {-1, 0, -1};
+    cudaError_t e = gm_try<GmTall>(a, 0, 530, pl);
+    if (e == cudaSuccess) e = gm_try<GmPair>(a, 1, 650, pl);
+    if (e == cudaSuccess) e = gm_try<GmWide>(a, 2, 340, pl);
+    return e == cudaSuccess && pl->shape < 0 ? cudaErrorInvalidConfiguration : e;
+}
+
+template <class S>
+cudaError_t gm_launch(const GemmMaps& maps, GemmArgs& a, int clusters, cudaStream_t st) {
+    gm_tiles<S>(a, clusters);
+    cudaLaunchAttribute at[2];
+    cudaLaunchConfig_t cfg = gm_config<S>(at, a.tiles < clusters ? a.tiles : clusters);
+    cfg.stream = st;
     cfg.numAttrs = pdl_on() ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_mlp_gemm<CG>, maps, a);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_mlp_gemm<S>, maps, a);
     note_launch();
     return e == cudaSuccess ? cudaGetLastError() : e;
 }
-
-// Pairs or single CTAs, by the busiest cluster's k-blocks: a pair's tile has four times a single CTA's
-// products on twice the tensor cores, in 1.6 times as long (a single CTA reads its operands from
-// shared memory as fast as that allows).
-struct GmPlan {
-    int cg, clusters;
-};
-cudaError_t gm_plan(GemmArgs& a, GmPlan* pl) {
-    int n1 = 0, n2 = 0;
-    cudaError_t e = gm_clusters<1>(&n1);
-    if (e == cudaSuccess) e = gm_clusters<2>(&n2);
-    if (e != cudaSuccess) return e;
-    const int64_t c1 = gm_cost(a, 1, n1), c2 = gm_cost(a, 2, n2);
-    pl->cg = 16 * c2 <= 10 * c1 ? 2 : 1;
-    pl->clusters = pl->cg == 2 ? n2 : n1;
-    return cudaSuccess;
-}
 cudaError_t gm_run(const GemmMaps& maps, GemmArgs& a, const GmPlan& pl, cudaStream_t st) {
-    return pl.cg == 2 ? gm_launch<2>(maps, a, pl.clusters, st) : gm_launch<1>(maps, a, pl.clusters, st);
+    switch (pl.shape) {
+        case 0: return gm_launch<GmTall>(maps, a, pl.clusters, st);
+        case 1: return gm_launch<GmPair>(maps, a, pl.clusters, st);
+    }
+    return gm_launch<GmWide>(maps, a, pl.clusters, st);
 }
 
 GemmProb gm_prob(int M, int N, int K, int kind, int amn, int bmn, int set, int out) {
@@ -676,9 +697,9 @@ GemmArgs gm_args(int nprob, int* err) {
     return a;
 }
 
-// operand stored [rows][inner] with the summed index inside: boxes of 64 k-elements and `box` rows
-bool map_k(CUtensorMap* m, const void* p, int rows, int inner, int box) {
-    return make_map_box(m, p, (uint64_t)inner, (uint64_t)rows, GM_BK, (uint32_t)box);
+// operand stored [rows][inner] with the summed index inside: boxes of 64 k-elements and 64 rows
+bool map_k(CUtensorMap* m, const void* p, int rows, int inner) {
+    return make_map_box(m, p, (uint64_t)inner, (uint64_t)rows, GM_BK, 64);
 }
 // operand stored [k][outputs]: boxes of 64 outputs and 64 k-elements
 bool map_mn(CUtensorMap* m, const void* p, int k, int outs) {
@@ -714,8 +735,8 @@ cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, con
     const cudaError_t e = gm_plan(a, &pl);
     if (e != cudaSuccess) return e;
     GemmMaps m = {};
-    if (!map_k(&m.a[0], x, T, C, 128) || !map_k(&m.b[0], Wg, F, C, 64 * pl.cg) || !map_k(&m.b[1], Wu, F, C, 64 * pl.cg) ||
-        !map_out(&m.o[0], h, T, F, false, 64 * pl.cg))
+    if (!map_k(&m.a[0], x, T, C) || !map_k(&m.b[0], Wg, F, C) || !map_k(&m.b[1], Wu, F, C) ||
+        !map_out(&m.o[0], h, T, F, false, pl.shape < 2 ? 128 : 64))
         return cudaErrorInvalidValue;
     return gm_run(m, a, pl, st);
 }
@@ -728,7 +749,7 @@ cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16
     const cudaError_t e = gm_plan(a, &pl);
     if (e != cudaSuccess) return e;
     GemmMaps m = {};
-    if (!map_k(&m.a[0], h, T, F, 128) || !map_k(&m.b[0], Wd, C, F, 128) || !map_out(&m.o[0], y, T, C, false, 128))
+    if (!map_k(&m.a[0], h, T, F) || !map_k(&m.b[0], Wd, C, F) || !map_out(&m.o[0], y, T, C, false, 128))
         return cudaErrorInvalidValue;
     return gm_run(m, a, pl, st);
 }
@@ -746,7 +767,7 @@ cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uin
     const cudaError_t e = gm_plan(a, &pl);
     if (e != cudaSuccess) return e;
     GemmMaps m = {};
-    if (!map_k(&m.a[0], dy, T, C, 128) || !map_mn(&m.b[0], Wd, C, F) || !map_mn(&m.a[1], dy, T, C) || !map_mn(&m.b[1], h, T, F) ||
+    if (!map_k(&m.a[0], dy, T, C) || !map_mn(&m.b[0], Wd, C, F) || !map_mn(&m.a[1], dy, T, C) || !map_mn(&m.b[1], h, T, F) ||
         !map_out(&m.o[0], dg, T, F, false, 64) || !map_out(&m.o[1], du, T, F, false, 64) ||
         !map_out(&m.o[2], dWd, C, F, f32 != 0, 128))
         return cudaErrorInvalidValue;
@@ -767,7 +788,7 @@ cudaError_t launch_mlp_dx_dw(int T, int C, int F, const uint16_t* x, const uint1
     const cudaError_t e = gm_plan(a, &pl);
     if (e != cudaSuccess) return e;
     GemmMaps m = {};
-    if (!map_k(&m.a[0], dg, T, F, 128) || !map_k(&m.a[1], du, T, F, 128) || !map_mn(&m.b[0], Wg, F, C) ||
+    if (!map_k(&m.a[0], dg, T, F) || !map_k(&m.a[1], du, T, F) || !map_mn(&m.b[0], Wg, F, C) ||
         !map_mn(&m.b[1], Wu, F, C) || !map_mn(&m.a[2], dg, T, F) || !map_mn(&m.a[3], du, T, F) || !map_mn(&m.b[2], x, T, C) ||
         !map_out(&m.o[0], dx, T, C, false, 128) || !map_out(&m.o[1], dWg, F, C, f32 != 0, 128) ||
         !map_out(&m.o[2], dWu, F, C, f32 != 0, 128))
