@@ -1083,19 +1083,22 @@ namespace {
 // `saved` and `workspace` of the gated feed-forward block
 struct MlpLayout {
     size_t h, pq, saved_total;                // saved: bf16 [T][F], then p and q (mlp_pq_bytes each)
-    size_t err, hs, dg, du, ws_total;         // workspace: h of a forward without `saved` where dg is
+    size_t err, cnt, hs, dg, du, part, ws_total;   // workspace: h of a forward without `saved` where dg is
 };
 
-MlpLayout mlp_layout(int64_t T, int F) {
+MlpLayout mlp_layout(int64_t T, int C, int F) {
     MlpLayout L;
     const size_t tf = al((size_t)T * F * 2);
     L.h = 0;
     L.pq = tf;
     L.saved_total = al(tf + 2 * mlp_pq_bytes(T, F));
     L.err = 0;
-    L.hs = L.dg = 256;
+    L.cnt = 256;
+    static_assert(256 + MLP_COUNTERS * 4 <= XHC_MLP_HEADER_BYTES, "counters in the header");
+    L.hs = L.dg = XHC_MLP_HEADER_BYTES;
     L.du = L.dg + tf;
-    L.ws_total = L.du + tf;
+    L.part = L.du + tf;
+    L.ws_total = L.part + al(mlp_small_part_bytes(T, C, F));
     return L;
 }
 
@@ -1119,7 +1122,7 @@ xhc_status xhc_mlp_saved_bytes(const xhc_mlp_config* cfg, int64_t T, size_t* byt
     const xhc_status s = mlp_check(cfg, T);
     if (s != XHC_OK) return s;
     if (!bytes) return XHC_ERR_INVALID_ARG;
-    *bytes = mlp_layout(T, cfg->F).saved_total;
+    *bytes = mlp_layout(T, cfg->C, cfg->F).saved_total;
     return XHC_OK;
 }
 
@@ -1127,7 +1130,7 @@ xhc_status xhc_mlp_workspace_bytes(const xhc_mlp_config* cfg, int64_t T, size_t*
     const xhc_status s = mlp_check(cfg, T);
     if (s != XHC_OK) return s;
     if (!bytes) return XHC_ERR_INVALID_ARG;
-    *bytes = mlp_layout(T, cfg->F).ws_total;
+    *bytes = mlp_layout(T, cfg->C, cfg->F).ws_total;
     return XHC_OK;
 }
 
@@ -1140,13 +1143,18 @@ xhc_status xhc_mlp_fwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
         !aligned16(saved) || !aligned16(workspace))
         return XHC_ERR_ALIGNMENT;
     const int C = cfg->C, F = cfg->F, T32 = (int)T;
-    const MlpLayout L = mlp_layout(T, F);
+    const MlpLayout L = mlp_layout(T, C, F);
     char *sv = (char*)saved, *ws = (char*)workspace;
     const cudaStream_t st = (cudaStream_t)stream;
     PdlScope pdl;
     pdl.set((size_t)T * (C + F) * 2, st);
     uint16_t* h = (uint16_t*)(sv ? sv + L.h : ws + L.hs);
     int* err = (int*)(ws + L.err);
+    if (mlp_small(T, C, F)) {
+        XHC_K("mlp_small", st, launch_mlp_small(T32, C, F, cfg->act, x, W->gate, W->up, W->down, h, sv ? sv + L.pq : nullptr, y,
+                                                (float*)(ws + L.part), (int*)(ws + L.cnt), err, st));
+        return XHC_OK;
+    }
     XHC_K("mlp_gate", st, launch_mlp_gate(T32, C, F, cfg->act, x, W->gate, W->up, h,
                                           sv ? sv + L.pq : nullptr, err, st));
     XHC_K("mlp_down", st, launch_mlp_down(T32, C, F, h, W->down, y, err, st));
@@ -1167,7 +1175,7 @@ xhc_status xhc_mlp_bwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
         !aligned16(workspace))
         return XHC_ERR_ALIGNMENT;
     const int C = cfg->C, F = cfg->F, T32 = (int)T;
-    const MlpLayout L = mlp_layout(T, F);
+    const MlpLayout L = mlp_layout(T, C, F);
     const char* sv = (const char*)saved;
     char* ws = (char*)workspace;
     const cudaStream_t st = (cudaStream_t)stream;

@@ -21,11 +21,9 @@
 // and u: the derivative comes from the fp32 g, and no activation is evaluated again.  p and q keep the upper
 // 24 bits of fp32 (three bytes; 2^-16): as bf16 their rounding would come on top of that of dg
 // and du (dx off by 2.9e-3 of itself instead of 2.4e-3), and the bytes hide under the products.
-#include <math.h>
-
 #include <type_traits>
 
-#include "k_tc.cuh"
+#include "k_mlp.cuh"
 
 namespace xhc {
 
@@ -87,47 +85,6 @@ struct GemmArgs {
     int64_t q_off;
 };
 
-// p and q lie in blocks of 32 rows and 8 columns, 24 bytes a row: the upper halves of a block's rows, 16 bytes
-// after 16 bytes, then the third bytes, 8 after 8.  The 32 lanes of an epilogue warp hold 32 rows of the same
-// columns and so write and read 512 and 256 contiguous bytes.
-constexpr int PQ_BLOCK = 32 * 24;
-__host__ __device__ __forceinline__ int64_t pq_at(int64_t row, int col, int F) {
-    return ((row >> 5) * (F / 8) + col / 8) * PQ_BLOCK;
-}
-// The upper 24 bits of 8 values (cut, not rounded: a carry could turn a NaN into another value)
-__device__ __forceinline__ void pq_store(unsigned char* blk, int lane, const float* v) {
-    uint32_t hi[4], lo[2];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) hi[e] = __byte_perm(__float_as_uint(v[2 * e]), __float_as_uint(v[2 * e + 1]), 0x7632);
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-        const uint32_t a = __byte_perm(__float_as_uint(v[4 * e]), __float_as_uint(v[4 * e + 1]), 0x0051);
-        const uint32_t b = __byte_perm(__float_as_uint(v[4 * e + 2]), __float_as_uint(v[4 * e + 3]), 0x0051);
-        lo[e] = __byte_perm(a, b, 0x5410);
-    }
-    *reinterpret_cast<uint4*>(blk + lane * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-    *reinterpret_cast<uint2*>(blk + 512 + lane * 8) = make_uint2(lo[0], lo[1]);
-}
-struct Pq8 {
-    uint4 hi;
-    uint2 lo;
-};
-__device__ __forceinline__ Pq8 pq_load(const unsigned char* blk, int lane) {
-    Pq8 r;
-    r.hi = ld_stream(blk + lane * 16);
-    asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(r.lo.x), "=r"(r.lo.y) : "l"(blk + 512 + lane * 8));
-    return r;
-}
-__device__ __forceinline__ void pq_unpack(const Pq8& r, float* v) {
-    const uint32_t hi[4] = {r.hi.x, r.hi.y, r.hi.z, r.hi.w}, lo[2] = {r.lo.x, r.lo.y};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        // bytes: 0, the low byte e of lo, the two of hi
-        const uint32_t l = __byte_perm(lo[e / 4], 0u, 0x4404u | ((uint32_t)(e & 3) << 4));
-        v[e] = __uint_as_float(__byte_perm(l, hi[e / 2], (e & 1) ? 0x7610 : 0x5410));
-    }
-}
-
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
@@ -188,30 +145,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t ta, float* v) {
         : "r"(ta));
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
-}
-
-// q = act(g), p = u act'(g) and h = q u of 8 columns; exponentials and quotients in the fast forms (2^-21 or
-// so), far below the stored precision.  Where an exponential overflows the sigmoid is 0, as it should be.
-template <int ACT>
-__device__ __forceinline__ void mlp_act8(const float* g, const float* u, float* p, float* q, float* h) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        float dq;
-        if (ACT == XHC_ACT_SILU) {
-            const float s = __fdividef(1.0f, 1.0f + __expf(-g[e]));
-            q[e] = g[e] * s;
-            dq = s + q[e] * (1.0f - s);
-        } else if (ACT == XHC_ACT_GELU) {
-            const float c = normcdff(g[e]);
-            q[e] = g[e] * c;
-            dq = c + g[e] * 0.3989422804f * __expf(-0.5f * g[e] * g[e]);
-        } else {
-            q[e] = g[e] > 0.f ? g[e] : g[e] != g[e] ? g[e] : 0.f;
-            dq = g[e] > 0.f ? 1.f : 0.f;
-        }
-        p[e] = u[e] * dq;
-        h[e] = u[e] * q[e];
-    }
 }
 
 struct GmTile {
@@ -306,6 +239,10 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
     cluster_sync();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    if (warp == 2 && lane < 11) {   // the first use of a map finds it there
+        const CUtensorMap* m = lane < 4 ? &maps.a[lane] : lane < 8 ? &maps.b[lane - 4] : &maps.o[lane - 8];
+        asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)m) : "memory");
+    }
     pdl_entry();
 
     auto give_up = [&](int code) {
@@ -480,7 +417,7 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
 #pragma unroll
                         for (int o = 0; o < 4; ++o) {
                             float p[8], q[8], h[8];
-                            mlp_act8<decltype(act)::value>(v + 8 * o, u + 8 * o, p, q, h);
+                            mlp_factors<decltype(act)::value>(v + 8 * o, u + 8 * o, p, q, h);
                             st_shared16(stage + (BN == 256 ? lane * 128 + (((o0 / 8 + o) ^ (lane & 7)) << 4)
                                                            : lane * 64 + ((o ^ ((lane >> 1) & 3)) << 4)),
                                         pack8(h));
@@ -669,7 +606,11 @@ cudaError_t gm_launch(const GemmMaps& maps, GemmArgs& a, int clusters, cudaStrea
     note_launch();
     return e == cudaSuccess ? cudaGetLastError() : e;
 }
-cudaError_t gm_run(const GemmMaps& maps, GemmArgs& a, const GmPlan& pl, cudaStream_t st) {
+// na, nb, no: maps that are set
+cudaError_t gm_run(GemmMaps& maps, GemmArgs& a, const GmPlan& pl, int na, int nb, int no, cudaStream_t st) {
+    for (int q = na; q < 4; ++q) maps.a[q] = maps.a[0];
+    for (int q = nb; q < 4; ++q) maps.b[q] = maps.b[0];
+    for (int q = no; q < 3; ++q) maps.o[q] = maps.o[0];
     switch (pl.shape) {
         case 0: return gm_launch<GmTall>(maps, a, pl.clusters, st);
         case 1: return gm_launch<GmPair>(maps, a, pl.clusters, st);
@@ -738,7 +679,7 @@ cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, con
     if (!map_k(&m.a[0], x, T, C) || !map_k(&m.b[0], Wg, F, C) || !map_k(&m.b[1], Wu, F, C) ||
         !map_out(&m.o[0], h, T, F, false, pl.shape < 2 ? 128 : 64))
         return cudaErrorInvalidValue;
-    return gm_run(m, a, pl, st);
+    return gm_run(m, a, pl, 1, 2, 1, st);
 }
 
 cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, int* err,
@@ -751,7 +692,7 @@ cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16
     GemmMaps m = {};
     if (!map_k(&m.a[0], h, T, F) || !map_k(&m.b[0], Wd, C, F) || !map_out(&m.o[0], y, T, C, false, 128))
         return cudaErrorInvalidValue;
-    return gm_run(m, a, pl, st);
+    return gm_run(m, a, pl, 1, 1, 1, st);
 }
 
 cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uint16_t* Wd, const uint16_t* h, const void* pq,
@@ -771,7 +712,7 @@ cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uin
         !map_out(&m.o[0], dg, T, F, false, 64) || !map_out(&m.o[1], du, T, F, false, 64) ||
         !map_out(&m.o[2], dWd, C, F, f32 != 0, 128))
         return cudaErrorInvalidValue;
-    return gm_run(m, a, pl, st);
+    return gm_run(m, a, pl, 2, 2, 3, st);
 }
 
 cudaError_t launch_mlp_dx_dw(int T, int C, int F, const uint16_t* x, const uint16_t* dg, const uint16_t* du,
@@ -794,7 +735,7 @@ cudaError_t launch_mlp_dx_dw(int T, int C, int F, const uint16_t* x, const uint1
         !map_out(&m.o[2], dWu, F, C, f32 != 0, 128))
         return cudaErrorInvalidValue;
     m.b[3] = m.b[2];
-    return gm_run(m, a, pl, st);
+    return gm_run(m, a, pl, 4, 4, 3, st);
 }
 
 }  // namespace xhc

@@ -1,0 +1,88 @@
+// Shared by the kernels of the gated feed-forward block: its kept factors p and q, and the activation.
+#pragma once
+
+#include <math.h>
+
+#include "k_tc.cuh"
+
+namespace xhc {
+
+namespace {
+
+// p and q lie in blocks of 32 rows and 8 columns, 24 bytes a row: the upper halves of a block's rows, 16 bytes
+// after 16 bytes, then the third bytes, 8 after 8.  The 32 lanes of an epilogue warp hold 32 rows of the same
+// columns and so write and read 512 and 256 contiguous bytes.
+constexpr int PQ_BLOCK = 32 * 24;
+__host__ __device__ __forceinline__ int64_t pq_at(int64_t row, int col, int F) {
+    return ((row >> 5) * (F / 8) + col / 8) * PQ_BLOCK;
+}
+// The upper 24 bits of 8 values (cut, not rounded: a carry could turn a NaN into another value)
+__device__ __forceinline__ void pq_store(unsigned char* blk, int lane, const float* v) {
+    uint32_t hi[4], lo[2];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) hi[e] = __byte_perm(__float_as_uint(v[2 * e]), __float_as_uint(v[2 * e + 1]), 0x7632);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+        const uint32_t a = __byte_perm(__float_as_uint(v[4 * e]), __float_as_uint(v[4 * e + 1]), 0x0051);
+        const uint32_t b = __byte_perm(__float_as_uint(v[4 * e + 2]), __float_as_uint(v[4 * e + 3]), 0x0051);
+        lo[e] = __byte_perm(a, b, 0x5410);
+    }
+    *reinterpret_cast<uint4*>(blk + lane * 16) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint2*>(blk + 512 + lane * 8) = make_uint2(lo[0], lo[1]);
+}
+struct Pq8 {
+    uint4 hi;
+    uint2 lo;
+};
+__device__ __forceinline__ Pq8 pq_load(const unsigned char* blk, int lane) {
+    Pq8 r;
+    r.hi = ld_stream(blk + lane * 16);
+    asm volatile("ld.global.v2.u32 {%0, %1}, [%2];" : "=r"(r.lo.x), "=r"(r.lo.y) : "l"(blk + 512 + lane * 8));
+    return r;
+}
+__device__ __forceinline__ void pq_unpack(const Pq8& r, float* v) {
+    const uint32_t hi[4] = {r.hi.x, r.hi.y, r.hi.z, r.hi.w}, lo[2] = {r.lo.x, r.lo.y};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        // bytes: 0, the low byte e of lo, the two of hi
+        const uint32_t l = __byte_perm(lo[e / 4], 0u, 0x4404u | ((uint32_t)(e & 3) << 4));
+        v[e] = __uint_as_float(__byte_perm(l, hi[e / 2], (e & 1) ? 0x7610 : 0x5410));
+    }
+}
+
+// one value of p or q, at row `row` and column `col`
+__device__ __forceinline__ void pq_put(unsigned char* pq, int row, int col, int F, float v) {
+    unsigned char* blk = pq + pq_at(row, col, F);
+    const uint32_t u = __float_as_uint(v);
+    *reinterpret_cast<uint16_t*>(blk + (row & 31) * 16 + (col & 7) * 2) = (uint16_t)(u >> 16);
+    blk[512 + (row & 31) * 8 + (col & 7)] = (unsigned char)(u >> 8);
+}
+
+// q = act(g), p = u act'(g) and h = q u of n columns; exponentials and quotients in the fast forms (2^-21 or
+// so), far below the stored precision.  Where an exponential overflows the sigmoid is 0, as it should be.
+template <int ACT, int n = 8>
+__device__ __forceinline__ void mlp_factors(const float* g, const float* u, float* p, float* q, float* h) {
+#pragma unroll
+    for (int e = 0; e < n; ++e) {
+        float dq;
+        if (ACT == XHC_ACT_SILU) {
+            const float s = __fdividef(1.0f, 1.0f + __expf(-g[e]));
+            q[e] = g[e] * s;
+            dq = s + q[e] * (1.0f - s);
+        } else if (ACT == XHC_ACT_GELU) {
+            const float c = normcdff(g[e]);
+            q[e] = g[e] * c;
+            dq = c + g[e] * 0.3989422804f * __expf(-0.5f * g[e] * g[e]);
+        } else {
+            q[e] = g[e] > 0.f ? g[e] : g[e] != g[e] ? g[e] : 0.f;
+            dq = g[e] > 0.f ? 1.f : 0.f;
+        }
+        p[e] = u[e] * dq;
+        h[e] = u[e] * q[e];
+    }
+}
+
+
+}  // namespace
+
+}  // namespace xhc

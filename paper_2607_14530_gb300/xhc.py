@@ -16,6 +16,7 @@ from . import build as _build
 
 MAX_GROUP = 4
 MAX_CONV = 3
+MLP_HEADER = 4096   # XHC_MLP_HEADER_BYTES
 
 MHC, FULL, FLASH = 0, 1, 2
 STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported", 3: "alignment", 4: "cuda error", 5: "timeout"}
@@ -614,9 +615,9 @@ class Mlp:
         return torch.empty(self.saved_bytes(T), dtype=torch.uint8, device=device)
 
     def alloc_workspace(self, T: int, device="cuda"):
-        """A `workspace` buffer (scratch of one call at a time), error word zeroed."""
+        """A `workspace` buffer (scratch of one call at a time), its header zeroed."""
         ws = torch.empty(self.workspace_bytes(T), dtype=torch.uint8, device=device)
-        ws[:256].zero_()
+        ws[:MLP_HEADER].zero_()
         return ws
 
     def shapes(self) -> dict:

@@ -5,7 +5,7 @@ import torch
 
 import op_refs as R
 from paper_2607_14530_gb300 import synth
-from paper_2607_14530_gb300.xhc import Mlp, XhcError
+from paper_2607_14530_gb300.xhc import MLP_HEADER, Mlp, XhcError
 from xhc_cases import Guarded
 
 pytestmark = pytest.mark.gpu
@@ -23,7 +23,7 @@ def inputs(T, C, F, seed=0):
 def poisoned(op, T):
     saved, ws = op.alloc_saved(T), op.alloc_workspace(T)
     saved.fill_(0xFF)       # NaN as bf16 and as fp32
-    ws[256:].fill_(0xFF)
+    ws[MLP_HEADER:].fill_(0xFF)
     return saved, ws
 
 
@@ -37,7 +37,7 @@ def run(op, x, P, dy, grad_dtype=BF, accumulate=False, start=None):
     op.forward(P, x, ws, saved=saved, y=y.t)
     op.backward(P, x, dy, {n: g.t for n, g in grads.items()}, saved, ws, dx=dx.t, accumulate=accumulate)
     torch.cuda.synchronize()
-    assert int(ws[:4].view(torch.int32)) == 0
+    assert bool((ws[:MLP_HEADER] == 0).all())   # no wait gave up, and the counters are back at zero
     assert y.intact() and dx.intact() and all(g.intact() for g in grads.values())
     return dict({n: g.t for n, g in grads.items()}, y=y.t, dx=dx.t)
 
@@ -46,7 +46,8 @@ def run(op, x, P, dy, grad_dtype=BF, accumulate=False, start=None):
 SHAPES = [(1, 8, 8), (1, 264, 712), (2, 64, 128), (3, 72, 136), (7, 512, 1032), (16, 256, 520), (17, 1024, 2816), (31, 264, 712),
           (32, 128, 64), (33, 128, 72), (64, 520, 1024), (65, 256, 384), (100, 2056, 264), (127, 512, 512), (128, 512, 512),
           (129, 264, 712), (255, 384, 1000), (256, 1024, 256), (257, 256, 2048), (333, 264, 712), (700, 512, 1544),
-          (1029, 2048, 1384), (2500, 1024, 2816)]
+          (1029, 2048, 1384), (2500, 1024, 2816), (1, 1024, 2816), (16, 2056, 1384), (17, 4096, 1032), (40, 1024, 2816), (64, 1544, 2056),
+          (65, 1024, 2816), (4099, 512, 1032), (1200, 4096, 264)]
 
 
 @pytest.mark.parametrize("T,C,F", SHAPES)
@@ -96,6 +97,20 @@ def test_fp32_gradients_written_and_accumulated(T, C, F):
     b = run(op, x, P, dy)
     for n in NAMES:   # and rounded once
         assert torch.equal(b[n], got[n].to(BF)), n
+
+
+@pytest.mark.parametrize("C,F", [(264, 712), (512, 1544), (4096, 1024)])
+def test_few_tokens_keep_their_bits_in_any_batch(C, F):
+    most = 64 if C * F >= 2 ** 21 else 16
+    x, P, _ = inputs(most, C, F, seed=2)
+    x, op = x.cuda(), Mlp(C, F)
+    ws = poisoned(op, most)[1]
+    want = op.forward(P, x, ws)
+    for T in (1, 2, 8, 15, 16, 17, 32, 33, 63):
+        if T <= most:
+            ws = poisoned(op, T)[1]
+            assert torch.equal(op.forward(P, x[:T], ws), want[:T]), T
+            assert torch.equal(op.forward(P, x[most - T:], ws), want[most - T:]), T
 
 
 def test_a_token_with_nan_stays_by_itself():
@@ -166,7 +181,7 @@ def test_refusals():
     with pytest.raises(XhcError, match="W_up"):
         op.forward({n: v for n, v in P.items() if n != "W_up"}, x, ws)
     with pytest.raises(XhcError, match="bytes"):
-        op.forward(P, torch.zeros(400, 64, dtype=BF, device="cuda"), ws)
+        op.forward(P, torch.zeros(20000, 64, dtype=BF, device="cuda"), ws)
     with pytest.raises(XhcError, match="alignment"):
         op.forward(P, torch.zeros(4 * 64 + 8, dtype=BF, device="cuda")[4:-4].view(4, 64), ws)
     with pytest.raises(XhcError, match="accumulated"):
