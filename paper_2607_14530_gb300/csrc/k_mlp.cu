@@ -21,6 +21,7 @@
 // and u: the derivative comes from the fp32 g, and no activation is evaluated again.  p and q keep the upper
 // 24 bits of fp32 (three bytes; 2^-16): as bf16 their rounding would come on top of that of dg
 // and du (dx off by 2.9e-3 of itself instead of 2.4e-3), and the bytes hide under the products.
+#include <atomic>
 #include <type_traits>
 
 #include "k_mlp.cuh"
@@ -561,15 +562,25 @@ struct GmPlan {
 // many fit, 76 pairs or 36 fours of 152 SMs), and the busiest one's clocks: `per` for a stage of 64
 // k-elements and GM_TILE_CLOCKS for a tile.
 template <class S>
-cudaError_t gm_try(GemmArgs& a, int shape, int per, GmPlan* best) {
-    const void* k = (const void*)k_mlp_gemm<S>;
-    cudaError_t e = smem_optin(k, S::SMEM);
+cudaError_t gm_fit(int* n) {
+    static std::atomic<int> fit[64];   // of a device, asked for once: the answer takes microseconds
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
+    const bool keep = dev >= 0 && dev < 64;
+    if (keep && (*n = fit[dev].load(std::memory_order_relaxed)) > 0) return cudaSuccess;
     cudaLaunchAttribute at[2];
     const cudaLaunchConfig_t cfg = gm_config<S>(at, device_sms() / S::CTAS);
-    int n = 0;
-    e = cudaOccupancyMaxActiveClusters(&n, k_mlp_gemm<S>, &cfg);
+    e = cudaOccupancyMaxActiveClusters(n, k_mlp_gemm<S>, &cfg);
+    if (e == cudaSuccess && keep) fit[dev].store(*n, std::memory_order_relaxed);
+    return e;
+}
+template <class S>
+cudaError_t gm_try(GemmArgs& a, int shape, int per, GmPlan* best) {
+    cudaError_t e = smem_optin((const void*)k_mlp_gemm<S>, S::SMEM);
     if (e != cudaSuccess) return e;
+    int n = 0;
+    if ((e = gm_fit<S>(&n)) != cudaSuccess) return e;
     if (n < 1) return cudaSuccess;
     gm_tiles<S>(a, n);
     const int nc = a.tiles < n ? a.tiles : n;

@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array
 from dataclasses import dataclass, field
 
 import torch
@@ -558,12 +559,12 @@ class Group:
 
 def _arg(t, name, dtype, shape=None):
     """The pointer of an operand: contiguous, of that type and shape, on the current CUDA device."""
-    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() < 0 or not t.is_contiguous():
         raise XhcError(f"{name} must be a contiguous {str(dtype)[6:]} CUDA tensor")
-    if shape is not None and tuple(t.shape) != shape:
+    if shape is not None and t.shape != shape:
         raise XhcError(f"{name} must be of shape {list(shape)}, got {list(t.shape)}")
-    if t.device.index != torch.cuda.current_device():
-        raise XhcError(f"{name} is on cuda:{t.device.index}, which is not the current device")
+    if t.get_device() != torch._C._cuda_getDevice():
+        raise XhcError(f"{name} is on cuda:{t.get_device()}, which is not the current device")
     return t.data_ptr()
 
 
@@ -729,6 +730,7 @@ class SumNorm:
         return dX
 
 
+_CLIP_TYPES = frozenset((torch.float32, torch.bfloat16))
 _clip_bytes = None
 
 
@@ -756,39 +758,44 @@ def clip_grads(grads, max_norm: float, scale: float = 1.0, eps: float = 1e-6, ou
                 raise XhcError("out must have the names of grads")
             out = [out[n] for n in names]
         grads = [grads[n] for n in names]
-    else:
-        grads = list(grads)
-        if out is not None:
-            out = list(out)
-            if len(out) != len(grads):
-                raise XhcError(f"{len(grads)} gradients and {len(out)} outputs")
+    grads = list(grads)
     if out is not None:
-        for q, (g, o) in enumerate(zip(grads, out)):
-            if (g is None) != (o is None) or (g is not None and (o.dtype is not g.dtype or o.shape != g.shape)):
-                raise XhcError(f"out[{q}] must be like its gradient")
+        out = list(out)
+        if [o is None for o in out] != [g is None for g in grads]:
+            raise XhcError("every gradient needs an output, and no other")
         out = [o for o in out if o is not None]
     grads = [g for g in grads if g is not None]
     n, device = len(grads), torch.cuda.current_device()
-    for what, ts in (("gradient", grads), ("output", out or ())):
+
+    def checked(ts, what):
+        """The pointers, sizes and types of a list of tensors."""
         for q, t in enumerate(ts):
-            if t.dtype not in (torch.float32, torch.bfloat16) or not t.is_cuda or not t.is_contiguous():
-                raise XhcError(f"{what} {q} must be a contiguous fp32 or bf16 CUDA tensor")
-            if t.device.index != device:
-                raise XhcError(f"{what} {q} is on cuda:{t.device.index}, which is not the current device")
-    ptrs = [t.data_ptr() for t in (grads if out is None else out)]
-    nonempty = [p for p, t in zip(ptrs, grads) if t.numel()]
-    if len(set(nonempty)) != len(nonempty):
-        raise XhcError("the same tensor is there twice")
-    I = ctypes.c_int64 * n
+            if t.get_device() != device or not t.is_contiguous():
+                raise XhcError(f"{what} {q} must be a contiguous CUDA tensor on the current device")
+        types = [t.dtype for t in ts]
+        if not _CLIP_TYPES.issuperset(types):
+            raise XhcError(f"every {what} must be an fp32 or bf16 tensor")
+        return [t.data_ptr() for t in ts], [t.numel() for t in ts], types
+
+    ptrs, numel, types = checked(grads, "gradient")
+    to = ptrs
+    if out is not None:
+        to, onumel, otypes = checked(out, "output")
+        if onumel != numel or otypes != types:
+            raise XhcError("every output must be like its gradient")
+    if len(set(to)) != n:   # empty tensors may share an address
+        seen = [p for p, k in zip(to, numel) if k]
+        if len(set(seen)) != len(seen):
+            raise XhcError("the same tensor is there twice")
     if norm is None:
         norm = torch.empty(1, dtype=torch.float32, device="cuda")
     if ws is None:
         ws = clip_workspace()
     elif _clip_bytes is None:
         clip_workspace("cpu")
-    _check(lib().xhc_clip_grads(n, I(*[t.data_ptr() for t in grads]), None if out is None else I(*ptrs),
-                                I(*[t.numel() for t in grads]),
-                                (ctypes.c_int * n)(*[1 if t.dtype is torch.bfloat16 else 0 for t in grads]),
-                                scale, max_norm, eps, _arg(norm, "norm", torch.float32, (1,)), _buffer(ws, "ws", _clip_bytes),
-                                _stream(stream)), "xhc_clip_grads")
+    a, c, d = array("q", ptrs), array("q", numel), array("i", [1 if t is torch.bfloat16 else 0 for t in types])
+    b = None if out is None else array("q", to)
+    _check(lib().xhc_clip_grads(n, a.buffer_info()[0], None if b is None else b.buffer_info()[0], c.buffer_info()[0],
+                                d.buffer_info()[0], scale, max_norm, eps, _arg(norm, "norm", torch.float32, (1,)),
+                                _buffer(ws, "ws", _clip_bytes), _stream(stream)), "xhc_clip_grads")
     return norm
