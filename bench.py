@@ -765,7 +765,7 @@ def run_stack(args, wl_name):
     import torch
     from torch import nn
     from paper_2607_14530_gb300 import build, synth, xhc
-    from paper_2607_14530_gb300.model import XhcStack
+    from paper_2607_14530_gb300.model import GatedMLP, RMSNorm, XhcStack, clip_grads_
 
     dev = torch.device("cuda", 0)
     torch.cuda.set_device(dev)
@@ -784,7 +784,15 @@ def run_stack(args, wl_name):
         def forward(self, x):
             return x * self.s.to(x.dtype)
 
-    stack = XhcStack(cfg, L, lambda l, t: Gain(), seed=seed).to(dev)
+    F = args.mlp_width
+
+    def sublayer(l, t):
+        """Of slot t of group l: a gain, or with --mlp-width the MLP slots' norm and feed-forward block."""
+        if F and (cfg.mlp_mask >> t) & 1:
+            return nn.Sequential(RMSNorm(cfg.C, cfg.eps_norm), GatedMLP(cfg.C, F, seed=seed + 7 * l + t))
+        return Gain()
+
+    stack = XhcStack(cfg, L, sublayer, seed=seed, final_norm=bool(F)).to(dev)
     hid = synth.normal_bf16_on((T, cfg.C), seed + 5, dev)
     dy = synth.normal_bf16_on((T, cfg.C), seed + 6, dev)
     stream = torch.cuda.current_stream()
@@ -792,7 +800,11 @@ def run_stack(args, wl_name):
     def stack_step():
         h = hid.detach().requires_grad_(True)
         y = stack(h)
+        if F:   # a whole step: gradients of this one alone, clipped
+            stack.zero_grad(set_to_none=True)
         y.backward(dy)
+        if F:
+            clip_grads_(stack, 1.0)
 
     def timed(fn, k):
         for _ in range(3):
@@ -827,7 +839,7 @@ def run_stack(args, wl_name):
     bare_ms = timed(bare_step, args.steps)
     # the parts of a stack step that are neither the library's group calls nor glue: the L x G
     # sublayers' own forward and backward, and the stream expansion and sum with their backward
-    gains = [Gain().to(dev) for _ in range(L * cfg.G)]
+    gains = [sublayer(l, t).to(dev) for l in range(L) for t in range(cfg.G)]
 
     def sublayer_step():
         for m in gains:
@@ -845,10 +857,13 @@ def run_stack(args, wl_name):
 
     es_ms = timed(expand_sum_step, args.steps)
     line = {"metric": "stack of groups through the autograd glue: tokens/s fwd+bwd", "unit": "tokens/s",
-            "workload": f"{L} groups of: {desc}; sublayers: scalar gains (bf16)", "tokens": T,
+            "workload": f"{L} groups of: {desc}; sublayers: " +
+            (f"MLP slots RMS norm and gated feed-forward of width {F}, others scalar gains; final norm, "
+             "gradients clipped" if F else "scalar gains (bf16)"), "tokens": T,
             "stack_ms": stack_ms, "value": T / (stack_ms / 1000.0),
             "bare_group_calls_ms": bare_ms, "sublayers_ms": sub_ms, "expand_sum_ms": es_ms,
-            "glue_overhead": (stack_ms - sub_ms - es_ms) / bare_ms - 1.0,
+            # (with --mlp-width the step also has the final norm and the clipping)
+            "glue_overhead": None if F else (stack_ms - sub_ms - es_ms) / bare_ms - 1.0,
             "note": "glue_overhead: the stack step less the sublayers' own work and the stream "
                     "expansion / sum, over the bare group calls, minus 1",
             "steps": args.steps, "dtype": "f32", "data": "synthetic"}
@@ -873,6 +888,8 @@ def main():
                     help="inference: forward-only prefill and decode legs; stack: a stack of groups "
                          "through the autograd glue (separate lines)")
     ap.add_argument("--groups", type=int, default=4, help="groups of the stack leg")
+    ap.add_argument("--mlp-width", type=int, default=0,
+                    help="stack leg: gated feed-forward sublayers of this width in the MLP slots (0: scalar gains)")
     ap.add_argument("--decode-batch", type=int, default=256)
     args = ap.parse_args()
     if args.warmup < 3 and args.impl == "xhc":

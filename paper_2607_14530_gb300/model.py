@@ -18,15 +18,22 @@ those steps for autograd; every step of the connection op itself runs in libxhc'
   gradient it receives in place when that tensor is the one the next group or the stream sum
   returned and no hook or retain_grad watches the state; any other incoming gradient is copied
   first.
-* ``XhcStack``: expansion, L groups, stream sum.
+* ``XhcStack``: expansion, L groups, stream sum, or with ``final_norm`` the RMS norm of that sum in one pass
+  (``SumNorm`` of xhc.py).
+* ``RMSNorm`` and ``GatedMLP``: the MLP sublayer of a group's M slots, e.g. ``nn.Sequential(RMSNorm(C),
+  GatedMLP(C, F))`` (``SumNorm`` with one stream, ``Mlp``).
+* ``clip_grads_``: the global norm of a model's gradients, and their clipping (xhc_clip_grads).
 """
 from __future__ import annotations
 
+import threading
+
 import torch
 from torch import nn
+from torch.autograd.function import once_differentiable
 
-from . import synth
-from .xhc import Config, Group
+from . import synth, xhc
+from .xhc import Config, Group, Mlp, SumNorm
 
 
 def _owned(t: torch.Tensor) -> torch.Tensor:
@@ -60,6 +67,104 @@ class StreamSum(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dy):
         return _owned(ctx.g.stream_expand(dy.contiguous())), None
+
+
+_scratch = threading.local()
+
+
+def _workspace(op, T: int, device):
+    """A workspace of ``op`` for this call: kept per device and stream in each host thread (calls on one
+    stream from one thread follow one another), and made anew in a capture, whose graph may be replayed beside others."""
+    if torch.cuda.is_current_stream_capturing():
+        return op.alloc_workspace(T, device=device)
+    kept = _scratch.__dict__.setdefault("kept", {})
+    key = (type(op), device, torch.cuda.current_stream(device).cuda_stream)
+    n = op.workspace_bytes(T)
+    ws = kept.get(key)
+    if ws is None or ws.numel() < n:
+        ws = kept[key] = op.alloc_workspace(T, device=device)
+    return ws
+
+
+class _MlpFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, Wg, Wu, Wd, op):
+        T = x.shape[0]
+        saved = op.alloc_saved(T, device=x.device)
+        y = op.forward({"W_gate": Wg, "W_up": Wu, "W_down": Wd}, x, _workspace(op, T, x.device), saved=saved)
+        ctx.save_for_backward(x, Wg, Wu, Wd)
+        ctx.op, ctx.saved = op, saved
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, Wg, Wu, Wd = ctx.saved_tensors
+        P = {"W_gate": Wg, "W_up": Wu, "W_down": Wd}
+        grads = {n: torch.empty_like(v) for n, v in P.items()}
+        dx = ctx.op.backward(P, x, dy.contiguous(), grads, ctx.saved, _workspace(ctx.op, x.shape[0], x.device))
+        return dx, grads["W_gate"], grads["W_up"], grads["W_down"], None
+
+
+class GatedMLP(nn.Module):
+    """The gated feed-forward block as a module: [T, C] bf16 to [T, C], weights bf16
+    (act(x W_gate^T) * (x W_up^T)) W_down^T.  With grad mode off nothing is kept for a backward."""
+
+    def __init__(self, C: int, F: int, act: str = "silu", seed: int = 0):
+        super().__init__()
+        self.op = Mlp(C, F, act)
+        for i, (n, s) in enumerate(self.op.shapes().items()):
+            self.register_parameter(n, nn.Parameter(synth.normal_bf16(s, seed * 1000003 + i, std=s[1] ** -0.5)))
+
+    def forward(self, x):
+        x = x.contiguous()
+        if torch.is_grad_enabled():
+            return _MlpFn.apply(x, self.W_gate, self.W_up, self.W_down, self.op)
+        P = {"W_gate": self.W_gate, "W_up": self.W_up, "W_down": self.W_down}
+        return self.op.forward(P, x, _workspace(self.op, x.shape[0], x.device))
+
+
+class _SumNormFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, X, w, op):
+        saved = op.alloc_saved(X.shape[0], device=X.device)
+        y = op.forward(w, X, saved=saved)
+        # of several streams the sum is in `saved` (and the groups change the state in place); one is read again
+        ctx.save_for_backward(*((w, X) if op.N == 1 else (w,)))
+        ctx.op, ctx.saved, ctx.shape = op, saved, X.shape
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        w, X = ctx.saved_tensors if ctx.op.N == 1 else (*ctx.saved_tensors, None)
+        dw = torch.empty_like(w)
+        dX = ctx.op.backward(w, X, dy.contiguous(), dw, ctx.saved, _workspace(ctx.op, dy.shape[0], dy.device))
+        return _owned(dX), dw, None
+
+
+class RMSNorm(nn.Module):
+    """RMS norm of the sum of N streams, [T, N, C] bf16 to [T, C] (N = 1: of a hidden vector, [T, C]); its
+    weight is fp32, at first one."""
+
+    def __init__(self, C: int, eps: float = 1e-5, N: int = 1):
+        super().__init__()
+        self.op = SumNorm(N, C, eps)
+        self.w = nn.Parameter(torch.ones(C))
+
+    def forward(self, x):
+        x = x.contiguous()
+        if torch.is_grad_enabled():
+            return _SumNormFn.apply(x, self.w, self.op)
+        return self.op.forward(self.w, x)
+
+
+def clip_grads_(params, max_norm: float, scale: float = 1.0) -> torch.Tensor:
+    """The norm of all gradients of ``params`` (a module, or parameters) times ``scale``, and every gradient
+    times scale * min(1, max_norm / (norm + 1e-6)), in place (xhc.clip_grads).  ``scale``: e.g. one over the
+    number of micro-batches or ranks whose gradients were added.  The norm stays on the device (fp32 [1])."""
+    params = params.parameters() if isinstance(params, nn.Module) else params
+    return xhc.clip_grads([p.grad for p in params], max_norm, scale=scale)
 
 
 class _GroupFn(torch.autograd.Function):
@@ -194,18 +299,20 @@ class XhcGroup(nn.Module):
 
 
 class XhcStack(nn.Module):
-    """Embedding output [T, C] -> N streams -> L groups -> sum of the streams [T, C]."""
+    """Embedding output [T, C] -> N streams -> L groups -> sum of the streams [T, C]; with ``final_norm``
+    the RMS norm of that sum (formed from the fp32 sum, in one pass)."""
 
-    def __init__(self, cfg: Config, n_groups: int, make_sublayer, seed: int = 0, **kw):
+    def __init__(self, cfg: Config, n_groups: int, make_sublayer, seed: int = 0, final_norm: bool = False, **kw):
         super().__init__()
         self.cfg = cfg
         self.groups = nn.ModuleList(
             XhcGroup(cfg, [make_sublayer(l, t) for t in range(cfg.G)], seed=seed + 97 * l, **kw)
             for l in range(n_groups))
+        self.final_norm = RMSNorm(cfg.C, cfg.eps_norm, cfg.N) if final_norm else None
 
     def forward(self, hidden):
         g = self.groups[0].g
         X = StreamExpand.apply(hidden, g)
         for grp in self.groups:
             X = grp(X)
-        return StreamSum.apply(X, g)
+        return StreamSum.apply(X, g) if self.final_norm is None else self.final_norm(X)

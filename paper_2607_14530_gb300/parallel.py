@@ -19,6 +19,8 @@ from __future__ import annotations
 import torch
 import torch.distributed as dist
 
+from .xhc import clip_grads
+
 
 def _rank_world(group):
     return dist.get_rank(group), dist.get_world_size(group)
@@ -90,11 +92,13 @@ class SequenceChunk:
     backward ``post_bwd(t)``, which returns the halo's gradient to the previous rank and adds the
     next rank's to this rank's d_out, then the sublayer's backward and ``pre_bwd(t)``.
     Parameter gradients are all-reduced by ``finish_backward`` (or by the caller's data-parallel
-    framework)."""
+    framework), and there clipped to ``max_norm`` if one is given: the ranks then hold the same gradients, so
+    each clips its own, and their norm stays in ``grad_norm``."""
 
     def __init__(self, g, B: int, S: int, group=None):
         self.g, self.B, self.S, self.group = g, B, S, group
         self.halos = {}
+        self.grad_norm = None
 
     def _conv(self, t):
         return self.g.cfg.K(t) > 1
@@ -122,5 +126,10 @@ class SequenceChunk:
     def pre_bwd(self, t, P, X, d_input, dX, grads, saved, ws, stream=None):
         self.g.pre_bwd(t, P, X, d_input, dX, grads, saved, ws, stream)
 
-    def finish_backward(self, grads: dict):
-        return allreduce_grads(grads, self.group)
+    def finish_backward(self, grads: dict, max_norm: float | None = None, scale: float = 1.0):
+        """The gradients summed over the ranks; with ``max_norm`` times ``scale`` (e.g. one over the number of
+        micro-batches) and clipped (xhc.clip_grads)."""
+        allreduce_grads(grads, self.group)
+        if max_norm is not None:
+            self.grad_norm = clip_grads(grads, max_norm, scale=scale)
+        return grads

@@ -1,0 +1,225 @@
+"""The operators together, as a model uses them: a stack of groups whose M slots hold a norm and a gated
+feed-forward block, a final norm over the streams, a training step that ends in clipping, and a decode step.
+
+The modules add no arithmetic: their results are, bit for bit, those of the library's calls issued by hand; the
+operators' own accuracy is tested apart."""
+import math
+
+import pytest
+import torch
+from torch import nn
+
+import op_refs as R
+from paper_2607_14530_gb300 import synth
+from paper_2607_14530_gb300.model import GatedMLP, RMSNorm, XhcStack, clip_grads_
+from paper_2607_14530_gb300.xhc import Config, Group, Mlp, SumNorm
+
+pytestmark = pytest.mark.gpu
+
+BF = torch.bfloat16
+T, F, L = 192, 200, 2
+CFG = Config.flash(8, 4, 2, 128, 4, seq_len=64)
+
+
+class Scale(nn.Module):
+    def forward(self, x):
+        return x * 0.125
+
+
+def sublayer(l, t):
+    if (CFG.mlp_mask >> t) & 1:
+        return nn.Sequential(RMSNorm(CFG.C), GatedMLP(CFG.C, F, seed=7 * l + t))
+    return Scale()
+
+
+def step(stack, h, dy):
+    hd = h.clone().requires_grad_(True)
+    y = stack(hd)
+    y.backward(dy)
+    return y.detach(), hd.grad
+
+
+def by_hand(stack, h, dy):
+    """The same step through the library's calls."""
+    g, C = Group(CFG), CFG.C
+    mlp, norm, last = Mlp(C, F), SumNorm(1, C), SumNorm(CFG.N, C, CFG.eps_norm)
+    grads, kept = {}, []
+    X = g.stream_expand(h)
+    ws = g.alloc_workspace(T)
+    for grp in stack.groups:
+        saved, P, per = g.alloc_saved(T), grp.param_dict(), []
+        for t in range(CFG.G):
+            inp = torch.empty(T, C, dtype=BF, device="cuda")
+            g.pre_fwd(t, P, X, inp, saved, ws)
+            if (CFG.mlp_mask >> t) & 1:
+                w, m = grp.sublayers[t][0].w.detach(), grp.sublayers[t][1]
+                W = {n: getattr(m, n).detach() for n in mlp.shapes()}
+                s1, s2 = norm.alloc_saved(T), mlp.alloc_saved(T)
+                u = norm.forward(w, inp, saved=s1)
+                out = mlp.forward(W, u, mlp.alloc_workspace(T), saved=s2)
+                per.append((inp, u, w, W, s1, s2, out))
+            else:
+                out = inp * 0.125
+                per.append((inp, None, None, None, None, None, out))
+            g.post_fwd(t, P, X, out, saved, ws)
+        kept.append((grp, saved, P, per))
+    s3 = last.alloc_saved(T)
+    w3 = stack.final_norm.w.detach()
+    y = last.forward(w3, X, saved=s3)
+    dw = torch.empty_like(w3)
+    dX = last.backward(w3, None, dy, dw, s3, last.alloc_workspace(T))
+    grads[stack.final_norm.w] = dw
+    for grp, saved, P, per in reversed(kept):
+        G = {n: torch.zeros_like(v) for n, v in P.items()}
+        for t in reversed(range(CFG.G)):
+            inp, u, w, W, s1, s2, out = per[t]
+            d_out = torch.empty_like(out)
+            g.post_bwd(t, P, X, dX, out, d_out, G, saved, ws)
+            if u is None:
+                d_in = d_out * 0.125
+            else:
+                gw = {n: torch.empty_like(v) for n, v in W.items()}
+                du = mlp.backward(W, u, d_out, gw, s2, mlp.alloc_workspace(T))
+                dw = torch.empty_like(w)
+                d_in = norm.backward(w, inp, du, dw, s1, norm.alloc_workspace(T))
+                grads[grp.sublayers[t][0].w] = dw
+                grads.update({getattr(grp.sublayers[t][1], n): v for n, v in gw.items()})
+            g.pre_bwd(t, P, X, d_in, dX, G, saved, ws)
+        grads.update({getattr(grp, n.replace(".", "_")): v for n, v in G.items()})
+    return y, g.stream_sum(dX), grads
+
+
+def make(seed):
+    stack = XhcStack(CFG, L, sublayer, seed=seed, final_norm=True).cuda()
+    return stack, synth.normal_bf16((T, CFG.C), seed + 5).cuda(), synth.normal_bf16((T, CFG.C), seed + 6).cuda()
+
+
+def test_training_step_with_clipping():
+    stack, h, dy = make(3)
+    y, dh = step(stack, h, dy)
+    want_y, want_dh, want = by_hand(stack, h, dy)
+    assert torch.equal(y, want_y) and torch.equal(dh, want_dh)
+    params = dict(stack.named_parameters())
+    assert len(want) == len(params)
+    for n, p in params.items():
+        assert torch.equal(p.grad, want[p]), n
+    before = [p.grad.clone() for p in params.values()]
+    norm, by, ref = R.clip([b.cpu() for b in before], 0.01, scale=0.5)
+    assert by < 0.5
+    got = clip_grads_(stack, 0.01, scale=0.5)
+    assert math.isclose(float(got), norm, rel_tol=2.0 ** -18)
+    for (n, p), r in zip(params.items(), ref):
+        last = R.BF if p.dtype is BF else R.F32
+        assert bool(((p.grad.cpu().double() - r).abs() <= (last + 2.0 ** -18) * r.abs() + 2.0 ** -133).all()), n
+    # again from the same state: the same bits, and gradients of two micro-batches add up
+    stack.zero_grad(set_to_none=True)
+    y2, dh2 = step(stack, h, dy)
+    assert torch.equal(y2, y) and torch.equal(dh2, dh)
+    assert all(torch.equal(p.grad, b) for p, b in zip(params.values(), before))
+
+
+def test_two_forwards_before_a_backward():
+    """Each call keeps its own forward state."""
+    stack, h, dy = make(4)
+    h2 = synth.normal_bf16((T, CFG.C), 99).cuda()
+    singles = []
+    for x in (h, h2):
+        stack.zero_grad(set_to_none=True)
+        singles.append((step(stack, x, dy), [p.grad.clone() for p in stack.parameters()]))
+    stack.zero_grad(set_to_none=True)
+    a, b = h.clone().requires_grad_(True), h2.clone().requires_grad_(True)
+    ya, yb = stack(a), stack(b)
+    torch.autograd.backward([ya, yb], [dy, dy])
+    assert torch.equal(ya, singles[0][0][0]) and torch.equal(yb, singles[1][0][0])
+    assert torch.equal(a.grad, singles[0][0][1]) and torch.equal(b.grad, singles[1][0][1])
+    for p, ga, gb in zip(stack.parameters(), singles[0][1], singles[1][1]):
+        # autograd's own sum, in one of the two orders
+        assert torch.equal(p.grad, ga + gb)
+
+
+def test_inference_and_other_streams():
+    stack, h, dy = make(5)
+    want = step(stack, h, dy)[0]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.no_grad():
+        assert torch.equal(stack(h), want)
+        with torch.cuda.stream(side):
+            other = stack(h)
+    side.synchronize()
+    assert torch.equal(other, want)
+
+
+def test_modules_in_captured_graphs():
+    """Two graphs of the same modules hold workspaces of their own: replayed at once on two streams, each gives
+    its own result."""
+    m = nn.Sequential(RMSNorm(256), GatedMLP(256, 520)).cuda()
+    xs = [synth.normal_bf16((n, 256), n).cuda() for n in (300, 24)]
+    with torch.no_grad():
+        want = [m(x) for x in xs]
+        graphs, outs = [], []
+        for x in xs:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                outs.append(m(x))
+            graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in xs]
+    for o in outs:
+        o.zero_()
+    torch.cuda.synchronize()
+    for _ in range(50):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
+
+
+def test_decode_step_with_the_block_as_sublayer():
+    """Decoding with norm and feed-forward block between pre_fwd and post_fwd_decode: a sequence's results do not
+    depend on the others in the batch, and equal the modules' on the same inputs."""
+    cfg = Config.flash(8, 4, 2, 128, 4)
+    g, mlp, norm = Group(cfg), Mlp(cfg.C, F), SumNorm(1, cfg.C)
+    P = {n: v.cuda() for n, v in synth.params(cfg.param_shapes(), 1).items()}
+    mods = [nn.Sequential(RMSNorm(cfg.C), GatedMLP(cfg.C, F, seed=t)).cuda() for t in range(cfg.G)]
+    X0 = synth.normal_bf16((12, cfg.N, cfg.C), 8).cuda()
+
+    def decode(rows, steps):
+        B = len(rows)
+        X, rings, pos = X0[rows].clone(), g.alloc_rings(B), torch.zeros(B, dtype=torch.int64, device="cuda")
+        saved, ws = g.alloc(B)
+        wm = mlp.alloc_workspace(B)
+        for _ in range(steps):
+            for t in range(cfg.G):
+                inp = torch.empty(B, cfg.C, dtype=BF, device="cuda")
+                g.pre_fwd(t, P, X, inp, saved, ws)
+                W = {n: getattr(mods[t][1], n).detach() for n in mlp.shapes()}
+                out = mlp.forward(W, norm.forward(mods[t][0].w.detach(), inp), wm)
+                with torch.no_grad():
+                    assert torch.equal(out, mods[t](inp))
+                g.post_fwd_decode(t, P, X, out, rings[t], pos, saved, ws)
+        torch.cuda.synchronize()
+        assert int(wm[:4].view(torch.int32)) == 0
+        return X
+
+    whole = decode(list(range(12)), 3)
+    for rows in ([0], [11], [3, 4, 5], list(range(2, 11))):
+        assert torch.equal(decode(rows, 3), whole[rows]), rows
+
+
+def test_gradients_of_the_modules():
+    """Against the 64-bit forms, through autograd: the block behind the norm."""
+    n, m = RMSNorm(264).cuda(), GatedMLP(264, 712, "gelu").cuda()
+    with torch.no_grad():
+        n.w.add_(0.1 * torch.randn(264, generator=torch.Generator().manual_seed(1)).cuda())
+    x = synth.normal_bf16((150, 264), 1).cuda().requires_grad_(True)
+    dy = synth.normal_bf16((150, 264), 2).cuda()
+    u = n(x)
+    u.retain_grad()
+    y = m(u)
+    y.backward(dy)
+    P = {k: getattr(m, k).detach() for k in m.op.shapes()}
+    ref = R.mlp(u.detach(), P, "gelu", dy)
+    R.assert_mlp(dict({k: getattr(m, k).grad for k in P}, y=y.detach(), dx=u.grad), ref)
+    ref = R.sum_norm(x.detach(), n.w.detach(), n.op.eps, u.grad)
+    R.assert_within({"y": u.detach(), "dX": x.grad, "dw": n.w.grad}, ref)

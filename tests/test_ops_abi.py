@@ -1,0 +1,111 @@
+"""Host-side checks of the operators around the connection op (no GPU: no call that passes them is made): the C
+ABI's refusals, with fake aligned addresses that are never dereferenced, and the binding's."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2607_14530_gb300 import build, parallel
+from paper_2607_14530_gb300 import xhc as X
+
+OK, INVALID, UNSUPPORTED, ALIGN = 0, 1, 2, 3
+A = [0x7f0000000000 + 4096 * i for i in range(16)]
+INF, NAN = float("inf"), float("nan")
+
+
+@pytest.fixture(scope="module")
+def L():
+    build.build()
+    return X.lib()
+
+
+def test_mlp_sizes_and_refusals(L):
+    n = ctypes.c_size_t()
+    size = lambda C, F, act, T: L.xhc_mlp_saved_bytes(X._MlpConfig(C, F, act), T, n)
+    assert size(64, 128, 0, 40) == OK
+    assert n.value >= 40 * 128 * 2 + 2 * 64 * 128 * 3   # h, and p and q of whole blocks of 32 tokens
+    assert L.xhc_mlp_workspace_bytes(X._MlpConfig(64, 128, 0), 40, n) == OK and n.value >= X.MLP_HEADER + 2 * 40 * 128 * 2
+    for bad in ((0, 128, 0, 1), (64, 0, 0, 1), (64, 128, 3, 1), (64, 128, -1, 1), (64, 128, 0, 0), (64, 128, 0, -5)):
+        assert size(*bad) == INVALID, bad
+    for bad in ((60, 128, 0, 1), (64, 132, 0, 1), (16392, 128, 0, 1), (64, 65544, 0, 1), (64, 128, 0, (1 << 24) + 1)):
+        assert size(*bad) == UNSUPPORTED, bad
+    assert size(16384, 65536, 2, 1 << 24) == OK
+    assert L.xhc_mlp_saved_bytes(None, 4, n) == INVALID and L.xhc_mlp_saved_bytes(X._MlpConfig(64, 128, 0), 4, None) == INVALID
+
+    c, W, G = X._MlpConfig(64, 128, 0), X._MlpWeights(A[0], A[1], A[2]), X._MlpWeights(A[3], A[4], A[5])
+    fwd = lambda W=W, x=A[6], y=A[7], s=None, ws=A[8], T=4: L.xhc_mlp_fwd(c, T, W, x, y, s, ws, None)
+    assert fwd(W=None) == INVALID and fwd(x=None) == INVALID and fwd(y=None) == INVALID and fwd(ws=None) == INVALID
+    assert fwd(W=X._MlpWeights(A[0], None, A[2])) == INVALID and fwd(T=0) == INVALID
+    assert fwd(x=A[6] + 8) == ALIGN and fwd(s=A[9] + 2) == ALIGN and fwd(W=X._MlpWeights(A[0], A[1] + 4, A[2])) == ALIGN
+    bwd = lambda g=G, dt=0, acc=0, dx=A[7], s=A[9], ws=A[8]: L.xhc_mlp_bwd(c, 4, W, A[6], A[10], dx, g, dt, acc, s, ws, None)
+    assert bwd(g=None) == INVALID and bwd(dt=2) == INVALID and bwd(acc=2) == INVALID and bwd(s=None) == INVALID
+    assert bwd(g=X._MlpWeights(A[3], A[4], None)) == INVALID and bwd(dt=1, acc=1) == UNSUPPORTED
+    assert bwd(dx=A[7] + 8) == ALIGN and bwd(g=X._MlpWeights(A[3], A[4], A[5] + 4)) == ALIGN
+
+
+def test_sum_norm_sizes_and_refusals(L):
+    n = ctypes.c_size_t()
+    assert L.xhc_sum_norm_saved_bytes(4, 64, 100, n) == OK and n.value == 512 + 100 * 64 * 4   # rstd, s
+    assert L.xhc_sum_norm_saved_bytes(1, 64, 100, n) == OK and n.value == 512
+    for bad in ((0, 64, 1), (1, 0, 1), (1, 64, 0)):
+        assert L.xhc_sum_norm_saved_bytes(*bad, n) == INVALID, bad
+    for bad in ((33, 64, 1), (1, 60, 1), (1, 16392, 1)):
+        assert L.xhc_sum_norm_saved_bytes(*bad, n) == UNSUPPORTED, bad
+    fwd = lambda N=2, eps=1e-5, T=4, x=A[0], w=A[1], y=A[2], s=None: L.xhc_sum_norm_fwd(N, 64, eps, T, x, w, y, s, None)
+    assert fwd(x=None) == INVALID and fwd(w=None) == INVALID and fwd(y=None) == INVALID and fwd(T=0) == INVALID
+    assert fwd(eps=-1.0) == INVALID and fwd(eps=NAN) == INVALID
+    assert fwd(x=A[0] + 8) == ALIGN and fwd(s=A[3] + 4) == ALIGN
+    bwd = lambda N=2, x=None, acc=0, s=A[3], dw=A[5]: L.xhc_sum_norm_bwd(N, 64, 4, x, A[1], A[2], A[4], dw, acc, s, A[6], None)
+    assert bwd(N=1) == INVALID and bwd(acc=-1) == INVALID and bwd(s=None) == INVALID and bwd(dw=None) == INVALID
+    assert bwd(dw=A[5] + 4) == ALIGN
+
+
+def test_clip_refusals(L):
+    P, I, D = ctypes.c_int64 * 2, ctypes.c_int64 * 2, ctypes.c_int * 2
+    call = lambda n=2, g=P(A[0], A[1]), o=None, k=I(8, 8), t=D(0, 1), scale=1.0, most=1.0, eps=1e-6, norm=A[2], ws=A[3]: (
+        L.xhc_clip_grads(n, g, o, k, t, scale, most, eps, norm, ws, None))
+    assert call(n=-1) == INVALID and call(g=None) == INVALID and call(k=None) == INVALID and call(t=None) == INVALID
+    assert call(ws=None) == INVALID and call(k=I(8, -1)) == INVALID and call(t=D(0, 2)) == INVALID
+    assert call(g=P(A[0], 0)) == INVALID and call(o=P(A[0], 0)) == INVALID
+    for bad in (dict(scale=INF), dict(scale=NAN), dict(most=-1.0), dict(most=NAN), dict(eps=-1.0), dict(eps=INF)):
+        assert call(**bad) == INVALID, bad
+    assert call(n=45001) == UNSUPPORTED and call(k=I(8, (1 << 40) + 1)) == UNSUPPORTED
+    assert call(g=P(A[0] + 2, A[1])) == ALIGN and call(o=P(A[0], A[1] + 1)) == ALIGN
+    assert call(ws=A[3] + 8) == ALIGN and call(norm=A[2] + 2) == ALIGN
+
+
+def test_binding_refuses_on_the_host():
+    with pytest.raises(X.XhcError, match="activation"):
+        X.Mlp(64, 128, "tanh")
+    with pytest.raises(X.XhcError, match="unsupported"):
+        X.Mlp(64, 132)
+    with pytest.raises(X.XhcError, match="unsupported"):
+        X.SumNorm(33, 64)
+    for eps in (-1e-5, NAN, INF):
+        with pytest.raises(X.XhcError, match="eps"):
+            X.SumNorm(1, 64, eps)
+    bf = torch.bfloat16
+    P = {n: torch.zeros(s, dtype=bf) for n, s in X.Mlp(64, 128).shapes().items()}
+    with pytest.raises(X.XhcError, match="CUDA tensor"):
+        X.Mlp(64, 128).forward(P, torch.zeros(4, 64, dtype=bf), None)
+    with pytest.raises(X.XhcError, match="CUDA tensor"):
+        X.SumNorm(2, 64).forward(torch.ones(64), torch.zeros(4, 2, 64, dtype=bf))
+
+
+def test_clip_outputs_have_to_match():
+    with pytest.raises(X.XhcError, match="names"):
+        X.clip_grads({"a": torch.ones(2)}, 1.0, out={"b": torch.ones(2)})
+    with pytest.raises(X.XhcError, match="output"):
+        X.clip_grads([torch.ones(2), None], 1.0, out=[None, torch.ones(2)])
+
+
+def test_finish_backward_clips_what_the_ranks_share(monkeypatch):
+    """The sums over the ranks are clipped, after the all-reduce, and only on demand."""
+    calls = []
+    monkeypatch.setattr(parallel, "allreduce_grads", lambda g, group=None: calls.append(("sum", group)) or g)
+    monkeypatch.setattr(parallel, "clip_grads", lambda g, most, scale=1.0: calls.append(("clip", most, scale)) or "norm")
+    chunk = parallel.SequenceChunk(None, 1, 1, group="ranks")
+    grads = {"a": torch.ones(2)}
+    assert chunk.finish_backward(grads) is grads and calls == [("sum", "ranks")] and chunk.grad_norm is None
+    assert chunk.finish_backward(grads, max_norm=2.0, scale=0.5) is grads
+    assert calls[1:] == [("sum", "ranks"), ("clip", 2.0, 0.5)] and chunk.grad_norm == "norm"
