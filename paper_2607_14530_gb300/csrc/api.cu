@@ -1083,22 +1083,21 @@ namespace {
 // `saved` and `workspace` of the gated feed-forward block
 struct MlpLayout {
     size_t h, pq, saved_total;                // saved: bf16 [T][F], then p and q (mlp_pq_bytes each)
-    size_t err, cnt, hs, dg, du, part, ws_total;   // workspace: h of a forward without `saved` where dg is
+    size_t err, cnt, hs, dg, du, ws_total;    // workspace: h of a forward without `saved` where dg is
 };
 
-MlpLayout mlp_layout(int64_t T, int C, int F) {
+MlpLayout mlp_layout(int64_t T, int F) {
     MlpLayout L;
     const size_t tf = al((size_t)T * F * 2);
     L.h = 0;
     L.pq = tf;
     L.saved_total = al(tf + 2 * mlp_pq_bytes(T, F));
     L.err = 0;
-    L.cnt = 256;
-    static_assert(256 + MLP_COUNTERS * 4 <= XHC_MLP_HEADER_BYTES, "counters in the header");
+    L.cnt = 64;
+    static_assert(64 + MLP_COUNTERS * 4 <= XHC_MLP_HEADER_BYTES, "counters in the header");
     L.hs = L.dg = XHC_MLP_HEADER_BYTES;
     L.du = L.dg + tf;
-    L.part = L.du + tf;
-    L.ws_total = L.part + al(mlp_small_part_bytes(T, C, F));
+    L.ws_total = L.du + tf;
     return L;
 }
 
@@ -1122,7 +1121,7 @@ xhc_status xhc_mlp_saved_bytes(const xhc_mlp_config* cfg, int64_t T, size_t* byt
     const xhc_status s = mlp_check(cfg, T);
     if (s != XHC_OK) return s;
     if (!bytes) return XHC_ERR_INVALID_ARG;
-    *bytes = mlp_layout(T, cfg->C, cfg->F).saved_total;
+    *bytes = mlp_layout(T, cfg->F).saved_total;
     return XHC_OK;
 }
 
@@ -1130,7 +1129,7 @@ xhc_status xhc_mlp_workspace_bytes(const xhc_mlp_config* cfg, int64_t T, size_t*
     const xhc_status s = mlp_check(cfg, T);
     if (s != XHC_OK) return s;
     if (!bytes) return XHC_ERR_INVALID_ARG;
-    *bytes = mlp_layout(T, cfg->C, cfg->F).ws_total;
+    *bytes = mlp_layout(T, cfg->F).ws_total;
     return XHC_OK;
 }
 
@@ -1143,7 +1142,7 @@ xhc_status xhc_mlp_fwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
         !aligned16(saved) || !aligned16(workspace))
         return XHC_ERR_ALIGNMENT;
     const int C = cfg->C, F = cfg->F, T32 = (int)T;
-    const MlpLayout L = mlp_layout(T, C, F);
+    const MlpLayout L = mlp_layout(T, F);
     char *sv = (char*)saved, *ws = (char*)workspace;
     const cudaStream_t st = (cudaStream_t)stream;
     PdlScope pdl;
@@ -1152,7 +1151,7 @@ xhc_status xhc_mlp_fwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
     int* err = (int*)(ws + L.err);
     if (mlp_small(T, C, F)) {
         XHC_K("mlp_small", st, launch_mlp_small(T32, C, F, cfg->act, x, W->gate, W->up, W->down, h, sv ? sv + L.pq : nullptr, y,
-                                                (float*)(ws + L.part), (int*)(ws + L.cnt), err, st));
+                                                (int*)(ws + L.cnt), err, st));
         return XHC_OK;
     }
     XHC_K("mlp_gate", st, launch_mlp_gate(T32, C, F, cfg->act, x, W->gate, W->up, h,
@@ -1175,7 +1174,7 @@ xhc_status xhc_mlp_bwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
         !aligned16(workspace))
         return XHC_ERR_ALIGNMENT;
     const int C = cfg->C, F = cfg->F, T32 = (int)T;
-    const MlpLayout L = mlp_layout(T, C, F);
+    const MlpLayout L = mlp_layout(T, F);
     const char* sv = (const char*)saved;
     char* ws = (char*)workspace;
     const cudaStream_t st = (cudaStream_t)stream;

@@ -1,4 +1,5 @@
-// Shared by the kernels of the gated feed-forward block: its kept factors p and q, and the activation.
+// Shared by the kernels of the gated feed-forward block: clusters, its kept factors p and q, and
+// the activation.
 #pragma once
 
 #include <math.h>
@@ -9,6 +10,20 @@ namespace xhc {
 
 namespace {
 
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the address of the same variable in CTA `rank` of the cluster
+__device__ __forceinline__ uint32_t map_rank(uint32_t a, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
+    return r;
+}
 // p and q lie in blocks of 32 rows and 8 columns, 24 bytes a row: the upper halves of a block's rows, 16 bytes
 // after 16 bytes, then the third bytes, 8 after 8.  The 32 lanes of an epilogue warp hold 32 rows of the same
 // columns and so write and read 512 and 256 contiguous bytes.

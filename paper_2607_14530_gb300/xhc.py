@@ -17,7 +17,7 @@ from . import build as _build
 
 MAX_GROUP = 4
 MAX_CONV = 3
-MLP_HEADER = 4096   # XHC_MLP_HEADER_BYTES
+MLP_HEADER = 256   # XHC_MLP_HEADER_BYTES
 
 MHC, FULL, FLASH = 0, 1, 2
 STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported", 3: "alignment", 4: "cuda error", 5: "timeout"}
