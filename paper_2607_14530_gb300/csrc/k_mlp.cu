@@ -5,17 +5,18 @@
 // One persistent kernel runs all of these products, several of them in a launch where none waits for another
 // (GemmProb: the backward takes dh with dW_down, then dx with dW_gate and dW_up).  A pair of CTAs on two SMs
 // takes 256 x BN outputs: each stages half of A's rows and half of B's, the MMA (cta_group::2) reads both
-// halves.  What bounds large products then is how fast the SMs are fed from L2: 32 KB an SM for each
-// 64 k-elements at BN = 256, 64 bytes a clock at the tensor cores' full rate, where about 50 arrive
-// (measured: a stage of 64 k-elements took 650 clocks instead of 512, and 490 instead of 256 with a
-// single CTA's 128 x 128 tile).  So two pairs form a cluster and share what they have in common, each CTA
-// loading half of it for both by TMA multicast (GmShape).
+// halves.  What bounds large products then is what a SM takes in: 32 KB for each 64 k-elements at BN = 256, 64 bytes
+// a clock at the tensor cores' full rate, where about 60 arrive (545 clocks a stage for 512 of products; a single
+// CTA's 128 x 128 tile would need 128 bytes a clock).  Two pairs can form a cluster and share what they have in common,
+// each CTA loading half of it for both by TMA multicast (GmShape), which halves the boxes to issue and the reads of L2.
+// The thread that issues the loads has 500 clocks for a stage too: boxes as large as possible, and a loop made for each
+// order of the operands (one loop that branched for every box: 3.65 ms for 3.51 of a training pass of
+// T = 8192, C = 4096, F = 11008, 198 us for 234 of the gate product of T = 4099, C = 2048, F = 5632 at BN = 128).
 // Operands arrive in the memory's own order: K-major where a row holds the summed index,
 // MN-major where it holds the output's (the weights in the input gradients, both operands of the weight
-// gradients), so nothing is transposed; every box is 64 x 64 elements (8 KB).  Warp 0 loads, warp 1 issues the MMAs, warps 2..9 read the
-// finished accumulator from TMEM, 32 rows and half of its columns each, and store through shared memory by
-// TMA, which also cuts off what a tile has past the output; two accumulators let that run under the next
-// tile's products.
+// gradients), so nothing is transposed.  Warp 0 loads, warp 1 issues the MMAs, warps 2..9 read the finished
+// accumulator from TMEM, 32 rows and half of its columns each, and store through shared memory by TMA, which also
+// cuts off what a tile has past the output; two accumulators let that run under the next tile's products.
 // Rounding: h, dg and du are stored as bf16 (once, from fp32): they are operands of the next product, whose
 // matrix instruction takes 16-bit ones.  The backward forms dg and du from p and q rather than from g
 // and u: the derivative comes from the fp32 g, and no activation is evaluated again.  p and q keep the upper
@@ -37,9 +38,9 @@ constexpr int GM_BOX = 64 * GM_BK * 2;          // bytes of a TMA box
 constexpr int GM_STORE = 4096;                  // staging bytes of an epilogue warp: 32 rows of 128 bytes
 
 // A cluster: PM x PN pairs of CTAs, 256 x BN outputs each.
-//   <2, 1, 256>  B shared: 24 KB an SM for 512 clocks of products
-//   <1, 1, 256>  nothing shared: 32 KB for 512 clocks; the GPU holds 152 SMs' worth of pairs, but 144 of fours
-//   <1, 2, 128>  A shared: 16 KB for 256 clocks; half of the first one's outputs a cluster, for smaller products
+//   <2, 1, 256>  B shared
+//   <1, 1, 256>  nothing shared; the GPU holds 152 SMs' worth of pairs, but 144 of fours
+//   <1, 2, 128>  A shared: 24 KB for 256 clocks of products, but twice the SMs for an output: for smaller products
 template <int PM_, int PN_, int BN_>
 struct GmShape {
     static constexpr int PM = PM_, PN = PN_, BN = BN_;
@@ -62,6 +63,11 @@ enum {
     GM_ADD      // added to fp32
 };
 
+// An operand's order: K-major, or MN-major, its boxes of one 64-output block or (MN_BLOCKS, where 64 divides the
+// row) of all blocks that a CTA loads.  The fewer boxes the better: K-major operands in boxes of 128 rows for 64
+// took the gate product of T = 4099, C = 2048, F = 5632 from 135 to 123 us.
+enum { K_MAJOR, MN_ROWS, MN_BLOCKS };
+
 struct GemmMaps {
     CUtensorMap a[4], b[4], o[3];
 };
@@ -72,7 +78,7 @@ struct GemmProb {
     int kb1, kb;       // k-blocks of the first operand pair, and of both
     int group;         // tile rows walked together
     int set, out;      // its first operand maps and output map
-    int kind, amn, bmn;
+    int kind, amn, bmn;   // the operands' order
 };
 struct GemmArgs {
     GemmProb p[3];
@@ -102,6 +108,19 @@ __device__ __forceinline__ void gm_load_mc(uint32_t dst, const CUtensorMap* map,
     asm volatile(
         "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster"
         " [%0], [%1, {%2, %3}], [%4], %5;" ::"r"(dst), "l"((uint64_t)map), "r"(x), "r"(y), "r"(bar), "h"(mask)
+        : "memory");
+}
+// the same of a map by blocks (map_blocks): rows from y on, blocks from z on
+__device__ __forceinline__ void gm_load3(uint32_t dst, const CUtensorMap* map, int y, int z, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes"
+        " [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"((uint64_t)map), "r"(0), "r"(y), "r"(z), "r"(bar)
+        : "memory");
+}
+__device__ __forceinline__ void gm_load3_mc(uint32_t dst, const CUtensorMap* map, int y, int z, uint32_t bar, uint16_t mask) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes.multicast::cluster"
+        " [%0], [%1, {%2, %3, %4}], [%5], %6;" ::"r"(dst), "l"((uint64_t)map), "r"(0), "r"(y), "r"(z), "r"(bar), "h"(mask)
         : "memory");
 }
 __device__ __forceinline__ void gm_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accum) {
@@ -241,47 +260,72 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
     if (warp == 0) {
         // ---------------- TMA producer ----------------
         if (lane == 0) {
-            const uint32_t lead = map_rank(full, (uint32_t)(rank & ~1));
+            const uint32_t lead = map_rank(full, (uint32_t)(rank & ~1)), ring = smem_u32(smem);
             const uint16_t mates = (uint16_t)(0x5u << half);   // this half's CTAs of both pairs
             int s = 0, issued = 0;
             uint32_t ph = 0;
-            for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
-                const GmTile tl = gm_tile(a, t);
-                const GemmProb& q = a.p[tl.p];
-                const int gate = q.kind == GM_GATE, amn = q.amn, bmn = q.bmn, kb1 = q.kb1, kbs = q.kb, set0 = q.set;
-                const int m0 = (tl.m * S::PM + pm) * 256 + half * 128;
-                // gate rows in the even CTA, up rows in the odd one: the halves of the accumulator's columns
-                const int n0 = gate ? (tl.n * S::PN + pn) * (BN / 2) : (tl.n * S::PN + pn) * BN + half * (BN / 2);
-                for (int kb = 0; kb < kbs; ++kb) {
+            // k-blocks 0 .. n - 1 of one operand pair; the operands' orders at compile time: this loop's own
+            // instructions are what a stage costs this thread
+            auto stream = [&](auto ao, auto bo, const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int n) {
+                constexpr int AO = decltype(ao)::value, BO = decltype(bo)::value;
+                auto load = [&](auto order, uint32_t dst, const CUtensorMap* m, int at, int k0, int blk, uint32_t bar, bool shared) {
+                    constexpr int O = decltype(order)::value;
+                    dst += blk * GM_BOX;
+                    if (O == MN_BLOCKS) {
+                        if (shared) gm_load3_mc(dst, m, k0, at / 64 + blk, bar, mates);
+                        else gm_load3(dst, m, k0, at / 64 + blk, bar);
+                    } else {
+                        const int x = O ? at + 64 * blk : k0, y = O ? k0 : at + 64 * blk;
+                        if (shared) gm_load_mc(dst, m, x, y, bar, mates);
+                        else gm_load(dst, m, x, y, bar);
+                    }
+                };
+                for (int k0 = 0; k0 < n * GM_BK; k0 += GM_BK) {
                     if (issued >= STAGES && !mbar_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
                         give_up(11);
-                        break;
+                        return;
                     }
-                    if (aborted()) break;
                     if (half == 0) mbar_expect_tx(full + 8 * s, 2 * S::STAGE);
-                    const int second = kb >= kb1 ? 1 : 0, set = set0 + second, k0 = (kb - (second ? kb1 : 0)) * GM_BK;
-                    const uint32_t sa = smem_u32(smem + s * S::STAGE), sb = sa + S::A_BYTES, bar = lead + 8 * s;
-                    const CUtensorMap *ma = &maps.a[set], *mb = &maps.b[gate ? half : set];
-                    // a box's place along the operand's 64-row blocks
-                    auto load = [&](uint32_t dst, const CUtensorMap* m, int mn, int at, int blk, bool shared) {
-                        const int x = mn ? at + 64 * blk : k0, y = mn ? k0 : at + 64 * blk;
-                        if (shared) gm_load_mc(dst + blk * GM_BOX, m, x, y, bar, mates);
-                        else gm_load(dst + blk * GM_BOX, m, x, y, bar);
-                    };
+                    const uint32_t sa = ring + (uint32_t)s * S::STAGE, sb = sa + S::A_BYTES, bar = lead + 8 * s;
                     if (S::PN > 1) {
-                        load(sa, ma, amn, m0, pair, true);
+                        load(ao, sa, ma, m0, k0, pair, bar, true);
                     } else {
-                        load(sa, ma, amn, m0, 0, false);
-                        load(sa, ma, amn, m0, 1, false);
+                        load(ao, sa, ma, m0, k0, 0, bar, false);
+                        if (AO == MN_ROWS) load(ao, sa, ma, m0, k0, 1, bar, false);
                     }
                     if (S::PM > 1) {
-                        load(sb, mb, bmn, n0, pair, true);
+                        load(bo, sb, mb, n0, k0, pair, bar, true);
                     } else {
-                        load(sb, mb, bmn, n0, 0, false);
-                        if (BN == 256) load(sb, mb, bmn, n0, 1, false);
+                        load(bo, sb, mb, n0, k0, 0, bar, false);
+                        if (BN == 256 && BO == MN_ROWS) load(bo, sb, mb, n0, k0, 1, bar, false);
                     }
                     ++issued;
                     if (++s == STAGES) { s = 0; ph ^= 1u; }
+                }
+            };
+            using K = std::integral_constant<int, K_MAJOR>;
+            using R = std::integral_constant<int, MN_ROWS>;
+            using Z = std::integral_constant<int, MN_BLOCKS>;
+            for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
+                const GmTile tl = gm_tile(a, t);
+                const GemmProb& q = a.p[tl.p];
+                const bool gate = q.kind == GM_GATE;
+                const int m0 = (tl.m * S::PM + pm) * 256 + half * 128;
+                // gate rows in the even CTA, up rows in the odd one: the halves of the accumulator's columns
+                const int n0 = gate ? (tl.n * S::PN + pn) * (BN / 2) : (tl.n * S::PN + pn) * BN + half * (BN / 2);
+                for (int set = q.set, n = q.kb1, left = q.kb; left > 0 && !aborted(); left -= n, n = left, ++set) {
+                    const CUtensorMap *ma = &maps.a[set], *mb = &maps.b[gate ? half : set];
+                    if (q.amn == K_MAJOR) {
+                        if (q.bmn == K_MAJOR) stream(K{}, K{}, ma, mb, m0, n0, n);
+                        else if (q.bmn == MN_ROWS) stream(K{}, R{}, ma, mb, m0, n0, n);
+                        else stream(K{}, Z{}, ma, mb, m0, n0, n);
+                    } else if (q.amn == MN_ROWS) {
+                        if (q.bmn == MN_ROWS) stream(R{}, R{}, ma, mb, m0, n0, n);
+                        else stream(R{}, Z{}, ma, mb, m0, n0, n);
+                    } else {
+                        if (q.bmn == MN_ROWS) stream(Z{}, R{}, ma, mb, m0, n0, n);
+                        else stream(Z{}, Z{}, ma, mb, m0, n0, n);
+                    }
                 }
             }
             if (!aborted()) {
@@ -313,6 +357,10 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
                 const uint32_t idesc = idesc_bf16(256, BN, amn) | ((bmn ? 1u : 0u) << 16);
                 // 16 k-elements on.  K-major: 32 bytes in the swizzled row; MN-major: 16 rows of 128 bytes
                 const uint32_t da = (amn ? 2048u : 32u) >> 4, db = (bmn ? 2048u : 32u) >> 4;
+                // of stage 0; the addresses of the others (18 bits, in 16 bytes) do not carry into the next field
+                const uint32_t sa = smem_u32(smem), sb = sa + S::A_BYTES;
+                const uint64_t a_desc = amn ? sw128_desc_mn(sa, GM_BOX) : sw128_desc(sa);
+                const uint64_t b_desc = bmn ? sw128_desc_mn(sb, GM_BOX) : sw128_desc(sb);
                 if (i >= 2 && !mbar_wait(accempty + 8 * buf, (uint32_t)((i >> 1) & 1) ^ 1u, a.wait_ns)) {
                     give_up(12);
                     break;
@@ -324,9 +372,7 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
                         break;
                     }
                     tc_fence_after();
-                    const uint32_t sa = smem_u32(smem + s * S::STAGE), sb = sa + S::A_BYTES;
-                    const uint64_t A = amn ? sw128_desc_mn(sa, GM_BOX) : sw128_desc(sa);
-                    const uint64_t B = bmn ? sw128_desc_mn(sb, GM_BOX) : sw128_desc(sb);
+                    const uint64_t A = a_desc + (uint64_t)((uint32_t)s * (S::STAGE >> 4)), B = b_desc + (uint64_t)((uint32_t)s * (S::STAGE >> 4));
 #pragma unroll
                     for (int kk = 0; kk < GM_BK / 16; ++kk)
                         gm_mma(tmem + (uint32_t)(buf * BN), A + (uint64_t)(kk * da), B + (uint64_t)(kk * db), idesc,
@@ -542,6 +588,8 @@ cudaLaunchConfig_t gm_config(cudaLaunchAttribute* at, int clusters) {
 struct GmPlan {
     int shape, clusters;
     int64_t clocks;
+    int a_rows() const { return shape == 2 ? 64 : 128; }   // rows of a K-major box: half of a shared operand's
+    int b_rows() const { return shape == 1 ? 128 : 64; }
 };
 
 // Clusters that the GPU holds at once (an SM without partners in its group of SMs takes none: the driver says how
@@ -586,9 +634,9 @@ cudaError_t gm_try(GemmArgs& a, int shape, int per, GmPlan* best) {
 
 cudaError_t gm_plan(GemmArgs& a, GmPlan* pl) {
     *pl = {-1, 0, -1};
-    cudaError_t e = gm_try<GmTall>(a, 0, 530, pl);
-    if (e == cudaSuccess) e = gm_try<GmPair>(a, 1, 650, pl);
-    if (e == cudaSuccess) e = gm_try<GmWide>(a, 2, 340, pl);
+    cudaError_t e = gm_try<GmTall>(a, 0, 545, pl);
+    if (e == cudaSuccess) e = gm_try<GmPair>(a, 1, 560, pl);
+    if (e == cudaSuccess) e = gm_try<GmWide>(a, 2, 440, pl);
     return e == cudaSuccess && pl->shape < 0 ? cudaErrorInvalidConfiguration : e;
 }
 
@@ -615,14 +663,12 @@ cudaError_t gm_run(GemmMaps& maps, GemmArgs& a, const GmPlan& pl, int na, int nb
     return gm_launch<GmWide>(maps, a, pl.clusters, st);
 }
 
-GemmProb gm_prob(int M, int N, int K, int kind, int amn, int bmn, int set, int out) {
+GemmProb gm_prob(int M, int N, int K, int kind, int set, int out) {
     GemmProb p = {};
     p.M = M;
     p.N = N;
     p.kb1 = p.kb = (K + GM_BK - 1) / GM_BK;
     p.kind = kind;
-    p.amn = amn;
-    p.bmn = bmn;
     p.set = set;
     p.out = out;
     return p;
@@ -635,12 +681,14 @@ GemmArgs gm_args(int nprob, int* err) {
     return a;
 }
 
-// operand stored [rows][inner] with the summed index inside: boxes of 64 k-elements and 64 rows
-bool map_k(CUtensorMap* m, const void* p, int rows, int inner) {
-    return make_map_box(m, p, (uint64_t)inner, (uint64_t)rows, GM_BK, 64);
+// operand stored [rows][inner] with the summed index inside: boxes of 64 k-elements and all the rows that a CTA loads
+bool map_k(CUtensorMap* m, const void* p, int rows, int inner, int box) {
+    return make_map_box(m, p, (uint64_t)inner, (uint64_t)rows, GM_BK, (uint32_t)box);
 }
-// operand stored [k][outputs]: boxes of 64 outputs and 64 k-elements
-bool map_mn(CUtensorMap* m, const void* p, int k, int outs) {
+// operand stored [k][outputs]: boxes of 64 k-elements and 64 outputs, or `outs` of them; `order` tells which
+bool map_mn(CUtensorMap* m, const void* p, int k, int outs, int box, int* order) {
+    *order = outs % 64 == 0 ? MN_BLOCKS : MN_ROWS;
+    if (*order == MN_BLOCKS) return map_blocks(m, p, (uint64_t)k, (uint64_t)outs, GM_BK, (uint32_t)box / 64);
     return make_map_box(m, p, (uint64_t)outs, (uint64_t)k, 64, GM_BK);
 }
 // output [rows][cols] of bf16 or fp32, stored 32 rows and `bytes` (64 or 128) of them at a time
@@ -665,7 +713,7 @@ size_t mlp_pq_bytes(int64_t T, int F) { return (size_t)((T + 31) / 32) * (F / 8)
 cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, const uint16_t* Wg, const uint16_t* Wu,
                             uint16_t* h, void* pq, int* err, cudaStream_t st) {
     GemmArgs a = gm_args(1, err);
-    a.p[0] = gm_prob(T, F, C, GM_GATE, 0, 0, 0, 0);
+    a.p[0] = gm_prob(T, F, C, GM_GATE, 0, 0);
     a.act = act;
     a.pq = (unsigned char*)pq;
     a.q_off = (int64_t)mlp_pq_bytes(T, F);
@@ -673,7 +721,7 @@ cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, con
     const cudaError_t e = gm_plan(a, &pl);
     if (e != cudaSuccess) return e;
     GemmMaps m = {};
-    if (!map_k(&m.a[0], x, T, C) || !map_k(&m.b[0], Wg, F, C) || !map_k(&m.b[1], Wu, F, C) ||
+    if (!map_k(&m.a[0], x, T, C, pl.a_rows()) || !map_k(&m.b[0], Wg, F, C, pl.b_rows()) || !map_k(&m.b[1], Wu, F, C, pl.b_rows()) ||
         !map_out(&m.o[0], h, T, F, false, pl.shape < 2 ? 128 : 64))
         return cudaErrorInvalidValue;
     return gm_run(m, a, pl, 1, 2, 1, st);
@@ -682,12 +730,12 @@ cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, con
 cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, int* err,
                             cudaStream_t st) {
     GemmArgs a = gm_args(1, err);
-    a.p[0] = gm_prob(T, C, F, GM_BF16, 0, 0, 0, 0);
+    a.p[0] = gm_prob(T, C, F, GM_BF16, 0, 0);
     GmPlan pl;
     const cudaError_t e = gm_plan(a, &pl);
     if (e != cudaSuccess) return e;
     GemmMaps m = {};
-    if (!map_k(&m.a[0], h, T, F) || !map_k(&m.b[0], Wd, C, F) || !map_out(&m.o[0], y, T, C, false, 128))
+    if (!map_k(&m.a[0], h, T, F, pl.a_rows()) || !map_k(&m.b[0], Wd, C, F, pl.b_rows()) || !map_out(&m.o[0], y, T, C, false, 128))
         return cudaErrorInvalidValue;
     return gm_run(m, a, pl, 1, 1, 1, st);
 }
@@ -695,17 +743,19 @@ cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16
 cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uint16_t* Wd, const uint16_t* h, const void* pq,
                               uint16_t* dg, uint16_t* du, void* dWd, int f32, int accumulate, int* err, cudaStream_t st) {
     GemmArgs a = gm_args(2, err);
-    const GemmProb dh = gm_prob(T, F, C, GM_DH, 0, 1, 0, 0);
-    const GemmProb dw = gm_prob(C, F, T, !f32 ? GM_BF16 : accumulate ? GM_ADD : GM_F32, 1, 1, 1, 2);
-    a.p[0] = dh.kb >= dw.kb ? dh : dw;   // the longer tiles first
-    a.p[1] = dh.kb >= dw.kb ? dw : dh;
+    const GemmProb dh = gm_prob(T, F, C, GM_DH, 0, 0);
+    const GemmProb dw = gm_prob(C, F, T, !f32 ? GM_BF16 : accumulate ? GM_ADD : GM_F32, 1, 2);
+    const int d = dh.kb >= dw.kb ? 0 : 1;   // the longer tiles first
+    a.p[d] = dh;
+    a.p[1 - d] = dw;
     a.pq = (unsigned char*)const_cast<void*>(pq);
     a.q_off = (int64_t)mlp_pq_bytes(T, F);
     GmPlan pl;
     const cudaError_t e = gm_plan(a, &pl);
     if (e != cudaSuccess) return e;
     GemmMaps m = {};
-    if (!map_k(&m.a[0], dy, T, C) || !map_mn(&m.b[0], Wd, C, F) || !map_mn(&m.a[1], dy, T, C) || !map_mn(&m.b[1], h, T, F) ||
+    if (!map_k(&m.a[0], dy, T, C, pl.a_rows()) || !map_mn(&m.b[0], Wd, C, F, pl.b_rows(), &a.p[d].bmn) ||
+        !map_mn(&m.a[1], dy, T, C, pl.a_rows(), &a.p[1 - d].amn) || !map_mn(&m.b[1], h, T, F, pl.b_rows(), &a.p[1 - d].bmn) ||
         !map_out(&m.o[0], dg, T, F, false, 64) || !map_out(&m.o[1], du, T, F, false, 64) ||
         !map_out(&m.o[2], dWd, C, F, f32 != 0, 128))
         return cudaErrorInvalidValue;
@@ -717,21 +767,23 @@ cudaError_t launch_mlp_dx_dw(int T, int C, int F, const uint16_t* x, const uint1
                              int accumulate, int* err, cudaStream_t st) {
     GemmArgs a = gm_args(3, err);
     const int kind = !f32 ? GM_BF16 : accumulate ? GM_ADD : GM_F32;
-    GemmProb d = gm_prob(T, C, F, GM_BF16, 0, 1, 0, 0);
+    GemmProb d = gm_prob(T, C, F, GM_BF16, 0, 0);
     d.kb = 2 * d.kb1;
     a.p[0] = d;
-    a.p[1] = gm_prob(F, C, T, kind, 1, 1, 2, 1);
-    a.p[2] = gm_prob(F, C, T, kind, 1, 1, 3, 2);
+    a.p[1] = gm_prob(F, C, T, kind, 2, 1);
+    a.p[2] = gm_prob(F, C, T, kind, 3, 2);
     GmPlan pl;
     const cudaError_t e = gm_plan(a, &pl);
     if (e != cudaSuccess) return e;
     GemmMaps m = {};
-    if (!map_k(&m.a[0], dg, T, F) || !map_k(&m.a[1], du, T, F) || !map_mn(&m.b[0], Wg, F, C) ||
-        !map_mn(&m.b[1], Wu, F, C) || !map_mn(&m.a[2], dg, T, F) || !map_mn(&m.a[3], du, T, F) || !map_mn(&m.b[2], x, T, C) ||
+    if (!map_k(&m.a[0], dg, T, F, pl.a_rows()) || !map_k(&m.a[1], du, T, F, pl.a_rows()) || !map_mn(&m.b[0], Wg, F, C, pl.b_rows(), &a.p[0].bmn) ||
+        !map_mn(&m.b[1], Wu, F, C, pl.b_rows(), &a.p[0].bmn) || !map_mn(&m.a[2], dg, T, F, pl.a_rows(), &a.p[1].amn) ||
+        !map_mn(&m.a[3], du, T, F, pl.a_rows(), &a.p[2].amn) || !map_mn(&m.b[2], x, T, C, pl.b_rows(), &a.p[1].bmn) ||
         !map_out(&m.o[0], dx, T, C, false, 128) || !map_out(&m.o[1], dWg, F, C, f32 != 0, 128) ||
         !map_out(&m.o[2], dWu, F, C, f32 != 0, 128))
         return cudaErrorInvalidValue;
     m.b[3] = m.b[2];
+    a.p[2].bmn = a.p[1].bmn;
     return gm_run(m, a, pl, 4, 4, 3, st);
 }
 

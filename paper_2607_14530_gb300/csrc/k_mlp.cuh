@@ -98,6 +98,20 @@ __device__ __forceinline__ void mlp_factors(const float* g, const float* u, floa
 }
 
 
+// A tensor [rows][inner], 64 dividing inner, as (64, rows, inner / 64): boxes of `box_rows` rows of `blocks` blocks of 64
+// elements, one block after the other in shared memory (what is past the last block or row reads as zero)
+bool map_blocks(CUtensorMap* m, const void* base, uint64_t rows, uint64_t inner, uint32_t box_rows, uint32_t blocks) {
+    auto enc = get_encode();
+    if (!enc) return false;
+    cuuint64_t gdim[3] = {64, rows, inner / 64};
+    cuuint64_t gstride[2] = {inner * 2, 128};
+    cuuint32_t box[3] = {64, box_rows, blocks};
+    cuuint32_t es[3] = {1, 1, 1};
+    return enc(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), gdim, gstride, box, es,
+               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 }  // namespace
 
 }  // namespace xhc

@@ -1,13 +1,16 @@
 // The feed-forward block's forward for few tokens (a decode step), in one launch:
 //   h = act(x W_gate^T) * (x W_up^T), then y = h W_down^T
-// It is bound by reading the weights once, 6 C F bytes.  The weights are the MMA's A operand (128 rows of
-// W_gate and of W_up, or of W_down, an M of 128 each), the tokens its N of 16 to 64: outputs transposed.
-// A cluster of four CTAs takes a weight tile, a quarter of its k-range each, through rings of 140 to 180 KB that keep
-// the memory busy.  The four partial sums meet in shared memory: the epilogue warp that holds rows 32 j .. 32 j + 31 of
-// a CTA's accumulator sends them to CTA j (st.async, which counts on j's barrier), and CTA j adds the four in
-// order and finishes these rows.  (Equal shares of the stream for every SM with the parts left in L2 and waited for by
-// counters took 59 us at C = 4096, F = 11008 and 27 at 24 tokens of C = 2048, F = 5632: every exchange is four trips
-// through L2.)  The cut depends on C and F alone: a token's bits do not depend on the other tokens or on their number.
+// It is bound by reading the weights once, 6 C F bytes.  The weights are the MMA's A operand (M = 128), the tokens its
+// N of 16 to 64: outputs transposed.  A tile is 64 outputs: of the first product 64 rows of W_gate above 64 of W_up;
+// of the second the same 64 rows of W_down at two neighbouring k-steps, each multiplied with both steps'
+// tokens, of which one half of the rows is used.  (Tiles of 128 outputs: 16 of them at C = 2048 left most SMs
+// without work in the second product, 26 us a call for 24 tokens of F = 5632.)
+// A cluster of four CTAs takes a tile, a quarter of its k-range each, through rings of 192 to 200 KB that keep
+// the memory busy.  The four partial sums meet in shared memory: the lanes that hold rows 16 j .. 16 j + 15 send
+// them to CTA j (st.async, which counts on j's barrier), and CTA j adds the four in order and finishes these
+// rows.  (Equal shares of the stream for every SM with the parts left in L2 and waited for by
+// counters took 59 us at C = 4096, F = 11008: every exchange is four trips through L2.)
+// The cut depends on C and F alone: a token's bits do not depend on the other tokens or on their number.
 // The second product needs all of h: the CTAs (one an SM, launched cooperatively, so all are there) meet at a
 // counter.  Loads of W_down do not need h and fill the ring before that wait, so the stream of weights
 // hardly stops between the products.
@@ -21,17 +24,18 @@ namespace {
 
 constexpr int SM_NT = 192;                   // warp 0 TMA, warp 1 MMA, warps 2..5 epilogue
 constexpr int SM_S = 4;                      // CTAs of a cluster
-constexpr int SM_A = 128 * 64 * 2;           // a box of 128 weight rows and 64 k-elements; two a stage
+constexpr int SM_BOX = 64 * 64 * 2;          // a box of 64 weight rows and 64 k-elements; two a stage
 constexpr int SM_ARRIVE = 0, SM_LEAVE = 1;   // counters
 
 template <int NT>
 struct SmShape {
-    static constexpr int B = NT * 64 * 2, STAGE = 2 * SM_A + 2 * B;
-    static constexpr int STAGES = NT == 16 ? 5 : NT == 32 ? 4 : 3;
+    static constexpr int B = NT * 64 * 2, STAGE = 2 * SM_BOX + 2 * B;
+    static constexpr int STAGES = NT == 16 ? 10 : NT == 32 ? 8 : 6;
     static constexpr int RT = NT < 32 ? NT : 32;            // tokens exchanged at a time
-    static constexpr int RECV = SM_S * RT * 32 * 8;         // [CTA][token][row] of (gate, up)
+    static constexpr int PART = 2 * RT * 16;                // floats of a CTA's part: [half][token][row]
+    static constexpr int RECV = SM_S * PART * 4;
     static constexpr int SMEM = STAGES * STAGE + 2 * RECV + (2 * STAGES + 7) * 8 + 16 + 1024;
-    static constexpr uint32_t COLS = 4 * NT;                // two accumulators of gate and up columns
+    static constexpr uint32_t COLS = 4 * NT;                // two accumulators of two times NT columns
 };
 
 // One of the two products: `tiles` weight tiles of `kb` stages; cluster c takes tiles c, c + clusters, ..., its CTA r
@@ -66,12 +70,6 @@ __device__ __forceinline__ void add_release(int* p) {
 __device__ __forceinline__ void send(uint32_t to, float a, uint32_t bar) {
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(to), "r"(__float_as_uint(a)), "r"(bar) : "memory");
 }
-__device__ __forceinline__ void send2(uint32_t to, float a, float b, uint32_t bar) {
-    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];" ::"r"(to), "r"(__float_as_uint(a)),
-                 "r"(__float_as_uint(b)), "r"(bar)
-                 : "memory");
-}
-
 template <int NT, int ACT>
 __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ SmMaps maps, const __grid_constant__ SmArgs a) {
     using S = SmShape<NT>;
@@ -132,17 +130,17 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
             uint32_t ph = 0;
             // the weights of k-step kb of tile m, or its tokens, into stage st
             auto load = [&](int f, int m, int kb, int st, bool weights) {
-                const uint32_t sa = smem_u32(smem + st * S::STAGE), sb = sa + 2 * SM_A, bar = full + 8 * st;
+                const uint32_t sa = smem_u32(smem + st * S::STAGE), sb = sa + 2 * SM_BOX, bar = full + 8 * st;
                 if (f == 0) {
                     if (weights) {
-                        tma_load_2d(sa, &maps.gate, kb * 64, m * 128, bar);
-                        tma_load_2d(sa + SM_A, &maps.up, kb * 64, m * 128, bar);
+                        tma_load_2d(sa, &maps.gate, kb * 64, m * 64, bar);
+                        tma_load_2d(sa + SM_BOX, &maps.up, kb * 64, m * 64, bar);
                     } else {
                         tma_load_2d(sb, &maps.x, kb * 64, 0, bar);
                     }
                 } else if (weights) {
-                    tma_load_2d(sa, &maps.down, kb * 128, m * 128, bar);
-                    tma_load_2d(sa + SM_A, &maps.down, kb * 128 + 64, m * 128, bar);
+                    tma_load_2d(sa, &maps.down, kb * 128, m * 64, bar);
+                    tma_load_2d(sa + SM_BOX, &maps.down, kb * 128 + 64, m * 64, bar);
                 } else {
                     tma_load_2d(sb, &maps.h, kb * 128, 0, bar);
                     tma_load_2d(sb + S::B, &maps.h, kb * 128 + 64, 0, bar);
@@ -187,7 +185,7 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
                             break;
                         }
                         if (aborted()) break;
-                        mbar_expect_tx(full + 8 * s, 2 * SM_A + (f ? 2 : 1) * S::B);
+                        mbar_expect_tx(full + 8 * s, 2 * SM_BOX + (f ? 2 : 1) * S::B);
                         load(f, m, kb, s, true);
                         ++ahead;
                         if (ready) tokens();
@@ -229,13 +227,12 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
                             break;
                         }
                         tc_fence_after();
-                        const uint32_t sa = smem_u32(smem + s * S::STAGE), sb = sa + 2 * SM_A;
+                        const uint32_t sa = smem_u32(smem + s * S::STAGE), sb = sa + 2 * SM_BOX;
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk) {
                             const uint32_t on = kb == 0 && kk == 0 ? 0u : 1u;
                             mma_bf16(d, sw128_desc(sa + kk * 32), sw128_desc(sb + kk * 32), idesc, on);
-                            if (f == 0) mma_bf16(d + NT, sw128_desc(sa + SM_A + kk * 32), sw128_desc(sb + kk * 32), idesc, on);
-                            else mma_bf16(d, sw128_desc(sa + SM_A + kk * 32), sw128_desc(sb + S::B + kk * 32), idesc, 1u);
+                            if (f) mma_bf16(d + NT, sw128_desc(sa + kk * 32), sw128_desc(sb + S::B + kk * 32), idesc, on);
                         }
                         mma_commit(empty + 8 * s);
                         if (++s == STAGES) { s = 0; ph ^= 1u; }
@@ -251,9 +248,10 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
     } else {
         // ---------------- epilogue (warps 2..5) ----------------
         const int quarter = warp & 3;
-        // rows 32 quarter .. + 31 of the accumulators go to CTA `quarter`, into this CTA's place of its buffers
-        const uint32_t to = map_rank(smem_u32(recv_mem), (uint32_t)quarter) + (uint32_t)(rank * RT * 32 * 8);
-        const uint32_t to_bar = map_rank(recv, (uint32_t)quarter);
+        // this lane's row of a half (gate or up; the first or the second k-step) goes to CTA row / 16, into this CTA's part
+        const int side = quarter >> 1, r64 = (quarter & 1) * 32 + lane;
+        const uint32_t to = map_rank(smem_u32(recv_mem), (uint32_t)(r64 >> 4)) + (uint32_t)(rank * S::PART + side * RT * 16 + (r64 & 15)) * 4;
+        const uint32_t to_bar = map_rank(recv, (uint32_t)(r64 >> 4));
         int seg = 0, round = 0;
         bool ok = true;
         // all four warps go on or none
@@ -269,27 +267,23 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
             int parts = 0;
             for (int r = 0; r < SM_S; ++r) parts += first_of(q, r) < first_of(q, r + 1) ? 1 : 0;
             for (int m = cl; m < q.tiles && ok; m += ncl) {
-                const uint32_t d = tmem + (uint32_t)((seg & 1) * 2 * NT) + ((uint32_t)(quarter * 32) << 16);
+                const uint32_t d = tmem + (uint32_t)((seg & 1) * 2 * NT + (f ? side * NT : 0)) + ((uint32_t)(quarter * 32) << 16);
                 const bool done = !part || mbar_wait(accfull + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1), a.wait_ns);
                 if (!done) give_up(26);
                 if (!(ok = agree(done))) break;
                 tc_fence_after();
-                const int row = m * 128 + rank * 32 + lane;   // that this CTA finishes
+                const int row = m * 64 + rank * 16 + (lane & 15);   // that this CTA finishes
                 for (int t0 = 0; t0 < a.T && ok; t0 += RT, ++round) {
                     const int b = round & 1, nt = min(RT, a.T - t0);
                     if (part) {
                         const uint32_t dst = to + (uint32_t)(b * S::RECV), bar = to_bar + 8 * b;
 #pragma unroll 1
                         for (int i = 0; i < nt; i += 16) {
-                            float v[16], u[16];
+                            float v[16];
                             tmem_ld16(d + t0 + i, v);
-                            if (f == 0) tmem_ld16(d + NT + t0 + i, u);
 #pragma unroll
                             for (int e = 0; e < 16; ++e)
-                                if (i + e < nt) {
-                                    if (f == 0) send2(dst + (uint32_t)((i + e) * 32 + lane) * 8, v[e], u[e], bar);
-                                    else send(dst + (uint32_t)((i + e) * 32 + lane) * 4, v[e], bar);
-                                }
+                                if (i + e < nt) send(dst + (uint32_t)(i + e) * 64, v[e], bar);
                         }
                         if (t0 + RT >= a.T) {   // the accumulator is read
                             tc_fence_before();
@@ -297,23 +291,18 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
                             if (lane == 0) mbar_arrive(accempty + 8 * (seg & 1));
                         }
                     }
-                    if (threadIdx.x == 64) mbar_expect_tx(recv + 8 * b, (uint32_t)(parts * nt * 32 * (f ? 4 : 8)));
+                    if (threadIdx.x == 64) mbar_expect_tx(recv + 8 * b, (uint32_t)(parts * nt * 2 * 16 * 4));
                     const bool got = mbar_wait(recv + 8 * b, (uint32_t)((round >> 1) & 1), a.wait_ns);
                     if (!got) give_up(27);
                     const float* in = reinterpret_cast<const float*>(recv_mem + b * S::RECV);
-                    for (int i = quarter; i < nt && got; i += 4) {
+                    for (int i = 2 * quarter + (lane >> 4); i < nt && got; i += 8) {
                         float v = 0.f, u = 0.f;
 #pragma unroll
                         for (int r = 0; r < SM_S; ++r) {
                             if (first_of(q, r) == first_of(q, r + 1)) continue;
-                            const float* at = in + r * RT * 32 * 2;
-                            if (f == 0) {
-                                const float2 x = reinterpret_cast<const float2*>(at)[i * 32 + lane];
-                                v += x.x;
-                                u += x.y;
-                            } else {
-                                v += at[i * 32 + lane];
-                            }
+                            const float* at = in + r * S::PART + i * 16 + (lane & 15);
+                            v += at[0];
+                            u += at[RT * 16];
                         }
                         const int t = t0 + i;
                         if (f == 0 && row < a.F) {
@@ -325,7 +314,7 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
                                 pq_put(a.pq + a.q_off, t, row, a.F, w);
                             }
                         } else if (f == 1 && row < a.C) {
-                            a.y[(int64_t)t * a.C + row] = f2bf(v);
+                            a.y[(int64_t)t * a.C + row] = f2bf(v + u);
                         }
                     }
                     // The buffer is read before any of these warps sends on.  With two buffers nothing more is
@@ -410,8 +399,8 @@ cudaError_t launch_mlp_small(int T, int C, int F, int act, const uint16_t* x, co
     a.T = T;
     a.C = C;
     a.F = F;
-    a.ph[0] = {(C + 63) / 64, (F + 127) / 128};
-    a.ph[1] = {(F + 127) / 128, (C + 127) / 128};
+    a.ph[0] = {(C + 63) / 64, (F + 63) / 64};
+    a.ph[1] = {(F + 127) / 128, (C + 63) / 64};
     a.cnt = cnt;
     a.h = h;
     a.y = y;
@@ -421,8 +410,8 @@ cudaError_t launch_mlp_small(int T, int C, int F, int act, const uint16_t* x, co
     a.err = err;
     const int NT = T <= 16 ? 16 : T <= 32 ? 32 : 64;
     SmMaps m;
-    if (!make_map_box(&m.gate, Wg, C, F, 64, 128) || !make_map_box(&m.up, Wu, C, F, 64, 128) ||
-        !make_map_box(&m.down, Wd, F, C, 64, 128) || !make_map_box(&m.x, x, C, T, 64, NT) || !make_map_box(&m.h, h, F, T, 64, NT))
+    if (!make_map_box(&m.gate, Wg, C, F, 64, 64) || !make_map_box(&m.up, Wu, C, F, 64, 64) ||
+        !make_map_box(&m.down, Wd, F, C, 64, 64) || !make_map_box(&m.x, x, C, T, 64, NT) || !make_map_box(&m.h, h, F, T, 64, NT))
         return cudaErrorInvalidValue;
     if (NT == 16) return sm_launch_act<16>(act, m, a, st);
     if (NT == 32) return sm_launch_act<32>(act, m, a, st);
