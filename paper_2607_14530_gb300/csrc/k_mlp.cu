@@ -10,8 +10,8 @@
 // CTA's 128 x 128 tile would need 128 bytes a clock).  Two pairs can form a cluster and share what they have in common,
 // each CTA loading half of it for both by TMA multicast (GmShape), which halves the boxes to issue and the reads of L2.
 // The thread that issues the loads has 500 clocks for a stage too: boxes as large as possible, and a loop made for each
-// order of the operands (one loop that branched for every box: 3.65 ms for 3.51 of a training pass of
-// T = 8192, C = 4096, F = 11008, 198 us for 234 of the gate product of T = 4099, C = 2048, F = 5632 at BN = 128).
+// order of the operands (one loop that branched for every box took 3.65 ms instead of 3.51 for a training pass of
+// T = 8192, C = 4096, F = 11008, and 234 us instead of 198 for the gate product of T = 4099, C = 2048, F = 5632 at BN = 128).
 // Operands arrive in the memory's own order: K-major where a row holds the summed index,
 // MN-major where it holds the output's (the weights in the input gradients, both operands of the weight
 // gradients), so nothing is transposed.  Warp 0 loads, warp 1 issues the MMAs, warps 2..9 read the finished

@@ -48,6 +48,7 @@ struct SmMaps {
 };
 struct SmArgs {
     int T, C, F;
+    int down_blocks;       // W_down and h in boxes of two k-steps (64 divides F)
     SmPhase ph[2];
     int* cnt;              // counters, zero between launches
     uint16_t *h, *y;
@@ -128,74 +129,91 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
         if (lane == 0) {
             int s = 0, issued = 0;
             uint32_t ph = 0;
-            // the weights of k-step kb of tile m, or its tokens, into stage st
-            auto load = [&](int f, int m, int kb, int st, bool weights) {
-                const uint32_t sa = smem_u32(smem + st * S::STAGE), sb = sa + 2 * SM_BOX, bar = full + 8 * st;
-                if (f == 0) {
-                    if (weights) {
-                        tma_load_2d(sa, &maps.gate, kb * 64, m * 64, bar);
-                        tma_load_2d(sa + SM_BOX, &maps.up, kb * 64, m * 64, bar);
-                    } else {
-                        tma_load_2d(sb, &maps.x, kb * 64, 0, bar);
+            const uint32_t ring = smem_u32(smem);
+            auto wait_h = [&]() {   // h is whole when every CTA has finished the first product
+                uint64_t t0 = 0;
+                for (uint32_t it = 0; ld_acquire(a.cnt + SM_ARRIVE) < (int)gridDim.x; ++it) {
+                    if ((it & 255u) != 255u) continue;   // reading the timer takes longer than a poll
+                    uint64_t now;
+                    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+                    if (t0 == 0) t0 = now;
+                    if (now - t0 > a.wait_ns || aborted()) {
+                        give_up(22);
+                        break;
                     }
-                } else if (weights) {
-                    tma_load_2d(sa, &maps.down, kb * 128, m * 64, bar);
-                    tma_load_2d(sa + SM_BOX, &maps.down, kb * 128 + 64, m * 64, bar);
-                } else {
-                    tma_load_2d(sb, &maps.h, kb * 128, 0, bar);
-                    tma_load_2d(sb + S::B, &maps.h, kb * 128 + 64, 0, bar);
                 }
+                asm volatile("fence.proxy.async;" ::: "memory");
             };
-            for (int f = 0; f < 2 && !aborted(); ++f) {
-                const SmPhase& q = a.ph[f];
-                const int k0 = first_of(q, rank), k1 = first_of(q, rank + 1);
-                // stages begun with their weights alone, oldest first: the second product's until h is there
-                int ahead = 0, st0 = s, am = cl, ak = k0;
-                bool ready = f == 0;
-                auto tokens = [&]() {   // their tokens
-                    for (; ahead > 0; --ahead) {
-                        load(f, am, ak, st0, false);
-                        if (++st0 == STAGES) st0 = 0;
-                        if (++ak == k1) { ak = k0; am += ncl; }
-                    }
-                };
-                auto wait_h = [&]() {   // h is whole when every CTA has finished the first product
-                    uint64_t t0 = 0;
-                    for (uint32_t it = 0; ld_acquire(a.cnt + SM_ARRIVE) < (int)gridDim.x; ++it) {
-                        if ((it & 255u) != 255u) continue;   // reading the timer takes longer than a poll
-                        uint64_t now;
-                        asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-                        if (t0 == 0) t0 = now;
-                        if (now - t0 > a.wait_ns || aborted()) {
-                            give_up(22);
-                            break;
-                        }
-                    }
-                    asm volatile("fence.proxy.async;" ::: "memory");
-                    ready = true;
-                };
-                for (int m = cl; m < q.tiles && k0 < k1 && !aborted(); m += ncl)
-                    for (int kb = k0; kb < k1; ++kb) {
-                        if (!ready && ahead == STAGES) {
-                            wait_h();
-                            tokens();
-                        }
-                        if (issued >= STAGES && !mbar_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
-                            give_up(21);
-                            break;
-                        }
-                        if (aborted()) break;
-                        mbar_expect_tx(full + 8 * s, 2 * SM_BOX + (f ? 2 : 1) * S::B);
-                        load(f, m, kb, s, true);
-                        ++ahead;
-                        if (ready) tokens();
-                        ++issued;
-                        if (++s == STAGES) { s = 0; ph ^= 1u; }
-                    }
-                if (ahead > 0) {   // (given up: loaded all the same, so that every stage begun is complete)
-                    if (!aborted()) wait_h();
-                    tokens();
+            // a free stage, told what it will receive
+            auto take = [&](int bytes) {
+                if (issued >= STAGES && !mbar_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
+                    give_up(21);
+                    return false;
                 }
+                mbar_expect_tx(full + 8 * s, bytes);
+                return true;
+            };
+            auto next = [&]() {
+                ++issued;
+                if (++s == STAGES) { s = 0; ph ^= 1u; }
+            };
+            {
+                const SmPhase& q = a.ph[0];
+                const int k0 = first_of(q, rank) * 64, k1 = first_of(q, rank + 1) * 64;
+                for (int m = cl; m < q.tiles && k0 < k1 && !aborted(); m += ncl)
+                    for (int k = k0; k < k1 && take(2 * SM_BOX + S::B); k += 64) {
+                        const uint32_t st = ring + (uint32_t)s * S::STAGE, bar = full + 8 * s;
+                        tma_load_2d(st, &maps.gate, k, m * 64, bar);
+                        tma_load_2d(st + SM_BOX, &maps.up, k, m * 64, bar);
+                        tma_load_2d(st + 2 * SM_BOX, &maps.x, k, 0, bar);
+                        next();
+                    }
+            }
+            if (!aborted()) {
+                const SmPhase& q = a.ph[1];
+                const int k0 = first_of(q, rank) * 128, k1 = first_of(q, rank + 1) * 128;
+                // W_down's boxes, and the tokens' once h is there: until then the ring fills with the weights alone
+                auto weights = [&](int m, int k) {
+                    const uint32_t st = ring + (uint32_t)s * S::STAGE, bar = full + 8 * s;
+                    if (a.down_blocks) {
+                        tma_load_3d(st, &maps.down, 0, m * 64, k / 64, bar);
+                    } else {
+                        tma_load_2d(st, &maps.down, k, m * 64, bar);
+                        tma_load_2d(st + SM_BOX, &maps.down, k + 64, m * 64, bar);
+                    }
+                };
+                auto tokens = [&](int at, int k) {
+                    const uint32_t st = ring + (uint32_t)at * S::STAGE + 2 * SM_BOX, bar = full + 8 * at;
+                    if (a.down_blocks) {
+                        tma_load_3d(st, &maps.h, 0, 0, k / 64, bar);
+                    } else {
+                        tma_load_2d(st, &maps.h, k, 0, bar);
+                        tma_load_2d(st + S::B, &maps.h, k + 64, 0, bar);
+                    }
+                };
+                const int s0 = s;
+                int ahead = 0, m = cl, k = k0;
+                for (; m < q.tiles && k0 < k1 && ahead < STAGES; ++ahead) {
+                    if (!take(2 * SM_BOX + 2 * S::B)) break;
+                    weights(m, k);
+                    next();
+                    if ((k += 128) == k1) { k = k0; m += ncl; }
+                }
+                if (ahead > 0) {
+                    if (!aborted()) wait_h();
+                    // (given up: loaded all the same, so that every stage begun is complete)
+                    for (int j = 0, at = s0, kt = k0; j < ahead; ++j) {
+                        tokens(at, kt);
+                        if (++at == STAGES) at = 0;
+                        if ((kt += 128) == k1) kt = k0;
+                    }
+                }
+                for (; m < q.tiles && k0 < k1 && !aborted(); m += ncl, k = k0)
+                    for (; k < k1 && take(2 * SM_BOX + 2 * S::B); k += 128) {
+                        weights(m, k);
+                        tokens(s, k);
+                        next();
+                    }
             }
             if (aborted()) {
                 // a wait ran out: the copies in flight land before this memory is given back
@@ -411,7 +429,11 @@ cudaError_t launch_mlp_small(int T, int C, int F, int act, const uint16_t* x, co
     const int NT = T <= 16 ? 16 : T <= 32 ? 32 : 64;
     SmMaps m;
     if (!make_map_box(&m.gate, Wg, C, F, 64, 64) || !make_map_box(&m.up, Wu, C, F, 64, 64) ||
-        !make_map_box(&m.down, Wd, F, C, 64, 64) || !make_map_box(&m.x, x, C, T, 64, NT) || !make_map_box(&m.h, h, F, T, 64, NT))
+        !make_map_box(&m.x, x, C, T, 64, NT))
+        return cudaErrorInvalidValue;
+    a.down_blocks = F % 64 == 0;
+    if (a.down_blocks ? !map_blocks(&m.down, Wd, C, F, 64, 2) || !map_blocks(&m.h, h, T, F, NT, 2)
+                      : !make_map_box(&m.down, Wd, F, C, 64, 64) || !make_map_box(&m.h, h, F, T, 64, NT))
         return cudaErrorInvalidValue;
     if (NT == 16) return sm_launch_act<16>(act, m, a, st);
     if (NT == 32) return sm_launch_act<32>(act, m, a, st);
