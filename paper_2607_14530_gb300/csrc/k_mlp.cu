@@ -6,12 +6,12 @@
 // (GemmProb: the backward takes dh with dW_down, then dx with dW_gate and dW_up).  A pair of CTAs on two SMs
 // takes 256 x BN outputs: each stages half of A's rows and half of B's, the MMA (cta_group::2) reads both
 // halves.  What bounds large products then is what a SM takes in: 32 KB for each 64 k-elements at BN = 256, 64 bytes
-// a clock at the tensor cores' full rate, where about 60 arrive (545 clocks a stage for 512 of products; a single
-// CTA's 128 x 128 tile would need 128 bytes a clock).  Two pairs can form a cluster and share what they have in common,
-// each CTA loading half of it for both by TMA multicast (GmShape), which halves the boxes to issue and the reads of L2.
-// The thread that issues the loads has 500 clocks for a stage too: boxes as large as possible, and a loop made for each
-// order of the operands (one loop that branched for every box took 3.65 ms instead of 3.51 for a training pass of
-// T = 8192, C = 4096, F = 11008, and 234 us instead of 198 for the gate product of T = 4099, C = 2048, F = 5632 at BN = 128).
+// a clock at the tensor cores' full rate, where 58 to 63 arrive (560 clocks a stage for 512 of products, 385 for 256 at
+// BN = 128; a single CTA's 128 x 128 tile would need 128 bytes a clock).  Two pairs can form a cluster and share what
+// they have in common, each CTA loading half of it for both by TMA multicast (GmShape), which halves the reads of L2.
+// The loading warp has these clocks for a stage too: boxes as large as possible, a loop made for each order of the
+// operands, and all its lanes in step (one loop that branched for every box, run by a single lane, took 3.65 ms instead
+// of 3.51 for a training pass of T = 8192, C = 4096, F = 11008, and 1540 us instead of 1071 for its gate product at BN = 128).
 // Operands arrive in the memory's own order: K-major where a row holds the summed index,
 // MN-major where it holds the output's (the weights in the input gradients, both operands of the weight
 // gradients), so nothing is transposed.  Warp 0 loads, warp 1 issues the MMAs, warps 2..9 read the finished
@@ -50,9 +50,6 @@ struct GmShape {
     static constexpr int SMEM = STAGES * STAGE + GM_EW * GM_STORE + (2 * STAGES + 5) * 8 + 16 + 1024;
     static constexpr int GROUP = 8 / PM;   // tile rows walked together: their B tiles are shared in L2
 };
-
-// Clocks that a tile costs beside its products, as far as they do not run under another's
-constexpr int GM_TILE_CLOCKS = 4000;
 
 // what becomes of an accumulator
 enum {
@@ -255,36 +252,36 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
         atomicExch(a.err, code);
         *(volatile int*)&s_abort = 1;
     };
-    auto aborted = [&]() { return *(volatile int*)&s_abort != 0; };
+    auto aborted = [&]() { return __any_sync(0xffffffffu, *(volatile int*)&s_abort != 0) != 0; };   // of a whole warp
 
     if (warp == 0) {
         // ---------------- TMA producer ----------------
-        if (lane == 0) {
-            const uint32_t lead = map_rank(full, (uint32_t)(rank & ~1)), ring = smem_u32(smem);
-            const uint16_t mates = (uint16_t)(0x5u << half);   // this half's CTAs of both pairs
-            int s = 0, issued = 0;
-            uint32_t ph = 0;
-            // k-blocks 0 .. n - 1 of one operand pair; the operands' orders at compile time: this loop's own
-            // instructions are what a stage costs this thread
-            auto stream = [&](auto ao, auto bo, const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int n) {
-                constexpr int AO = decltype(ao)::value, BO = decltype(bo)::value;
-                auto load = [&](auto order, uint32_t dst, const CUtensorMap* m, int at, int k0, int blk, uint32_t bar, bool shared) {
-                    constexpr int O = decltype(order)::value;
-                    dst += blk * GM_BOX;
-                    if (O == MN_BLOCKS) {
-                        if (shared) gm_load3_mc(dst, m, k0, at / 64 + blk, bar, mates);
-                        else gm_load3(dst, m, k0, at / 64 + blk, bar);
-                    } else {
-                        const int x = O ? at + 64 * blk : k0, y = O ? k0 : at + 64 * blk;
-                        if (shared) gm_load_mc(dst, m, x, y, bar, mates);
-                        else gm_load(dst, m, x, y, bar);
-                    }
-                };
-                for (int k0 = 0; k0 < n * GM_BK; k0 += GM_BK) {
-                    if (issued >= STAGES && !mbar_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
-                        give_up(11);
-                        return;
-                    }
+        const uint32_t lead = map_rank(full, (uint32_t)(rank & ~1)), ring = smem_u32(smem);
+        const uint16_t mates = (uint16_t)(0x5u << half);   // this half's CTAs of both pairs
+        int s = 0, issued = 0;
+        uint32_t ph = 0;
+        // k-blocks 0 .. n - 1 of one operand pair; the operands' orders at compile time: this loop's own
+        // instructions are what a stage costs this thread
+        auto stream = [&](auto ao, auto bo, const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int n) {
+            constexpr int AO = decltype(ao)::value, BO = decltype(bo)::value;
+            auto load = [&](auto order, uint32_t dst, const CUtensorMap* m, int at, int k0, int blk, uint32_t bar, bool shared) {
+                constexpr int O = decltype(order)::value;
+                dst += blk * GM_BOX;
+                if (O == MN_BLOCKS) {
+                    if (shared) gm_load3_mc(dst, m, k0, at / 64 + blk, bar, mates);
+                    else gm_load3(dst, m, k0, at / 64 + blk, bar);
+                } else {
+                    const int x = O ? at + 64 * blk : k0, y = O ? k0 : at + 64 * blk;
+                    if (shared) gm_load_mc(dst, m, x, y, bar, mates);
+                    else gm_load(dst, m, x, y, bar);
+                }
+            };
+            for (int k0 = 0; k0 < n * GM_BK; k0 += GM_BK) {
+                if (issued >= STAGES && !warp_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
+                    give_up(11);
+                    return;
+                }
+                if (elect_one()) {
                     if (half == 0) mbar_expect_tx(full + 8 * s, 2 * S::STAGE);
                     const uint32_t sa = ring + (uint32_t)s * S::STAGE, sb = sa + S::A_BYTES, bar = lead + 8 * s;
                     if (S::PN > 1) {
@@ -299,55 +296,56 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
                         load(bo, sb, mb, n0, k0, 0, bar, false);
                         if (BN == 256 && BO == MN_ROWS) load(bo, sb, mb, n0, k0, 1, bar, false);
                     }
-                    ++issued;
-                    if (++s == STAGES) { s = 0; ph ^= 1u; }
                 }
-            };
-            using K = std::integral_constant<int, K_MAJOR>;
-            using R = std::integral_constant<int, MN_ROWS>;
-            using Z = std::integral_constant<int, MN_BLOCKS>;
-            for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
-                const GmTile tl = gm_tile(a, t);
-                const GemmProb& q = a.p[tl.p];
-                const bool gate = q.kind == GM_GATE;
-                const int m0 = (tl.m * S::PM + pm) * 256 + half * 128;
-                // gate rows in the even CTA, up rows in the odd one: the halves of the accumulator's columns
-                const int n0 = gate ? (tl.n * S::PN + pn) * (BN / 2) : (tl.n * S::PN + pn) * BN + half * (BN / 2);
-                for (int set = q.set, n = q.kb1, left = q.kb; left > 0 && !aborted(); left -= n, n = left, ++set) {
-                    const CUtensorMap *ma = &maps.a[set], *mb = &maps.b[gate ? half : set];
-                    if (q.amn == K_MAJOR) {
-                        if (q.bmn == K_MAJOR) stream(K{}, K{}, ma, mb, m0, n0, n);
-                        else if (q.bmn == MN_ROWS) stream(K{}, R{}, ma, mb, m0, n0, n);
-                        else stream(K{}, Z{}, ma, mb, m0, n0, n);
-                    } else if (q.amn == MN_ROWS) {
-                        if (q.bmn == MN_ROWS) stream(R{}, R{}, ma, mb, m0, n0, n);
-                        else stream(R{}, Z{}, ma, mb, m0, n0, n);
-                    } else {
-                        if (q.bmn == MN_ROWS) stream(Z{}, R{}, ma, mb, m0, n0, n);
-                        else stream(Z{}, Z{}, ma, mb, m0, n0, n);
-                    }
+                __syncwarp();
+                ++issued;
+                if (++s == STAGES) { s = 0; ph ^= 1u; }
+            }
+        };
+        using K = std::integral_constant<int, K_MAJOR>;
+        using R = std::integral_constant<int, MN_ROWS>;
+        using Z = std::integral_constant<int, MN_BLOCKS>;
+        for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
+            const GmTile tl = gm_tile(a, t);
+            const GemmProb& q = a.p[tl.p];
+            const bool gate = q.kind == GM_GATE;
+            const int m0 = (tl.m * S::PM + pm) * 256 + half * 128;
+            // gate rows in the even CTA, up rows in the odd one: the halves of the accumulator's columns
+            const int n0 = gate ? (tl.n * S::PN + pn) * (BN / 2) : (tl.n * S::PN + pn) * BN + half * (BN / 2);
+            for (int set = q.set, n = q.kb1, left = q.kb; left > 0 && !aborted(); left -= n, n = left, ++set) {
+                const CUtensorMap *ma = &maps.a[set], *mb = &maps.b[gate ? half : set];
+                if (q.amn == K_MAJOR) {
+                    if (q.bmn == K_MAJOR) stream(K{}, K{}, ma, mb, m0, n0, n);
+                    else if (q.bmn == MN_ROWS) stream(K{}, R{}, ma, mb, m0, n0, n);
+                    else stream(K{}, Z{}, ma, mb, m0, n0, n);
+                } else if (q.amn == MN_ROWS) {
+                    if (q.bmn == MN_ROWS) stream(R{}, R{}, ma, mb, m0, n0, n);
+                    else stream(R{}, Z{}, ma, mb, m0, n0, n);
+                } else {
+                    if (q.bmn == MN_ROWS) stream(Z{}, R{}, ma, mb, m0, n0, n);
+                    else stream(Z{}, Z{}, ma, mb, m0, n0, n);
                 }
             }
-            if (!aborted()) {
-                // the MMAs' releases of the last stages reach every CTA of the cluster before one ends
-                for (int q = 0; q < STAGES; ++q) {
-                    if (issued + q >= STAGES && !mbar_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
-                        give_up(15);
-                        break;
-                    }
-                    if (++s == STAGES) { s = 0; ph ^= 1u; }
+        }
+        if (!aborted()) {
+            // the MMAs' releases of the last stages reach every CTA of the cluster before one ends
+            for (int q = 0; q < STAGES; ++q) {
+                if (issued + q >= STAGES && !warp_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
+                    give_up(15);
+                    break;
                 }
-            } else if (half == 0) {
-                // a wait ran out: the copies in flight land before this memory is given back
-                for (int q = 0; q < STAGES && q < issued; ++q) {
-                    if (--s < 0) { s = STAGES - 1; ph ^= 1u; }
-                    mbar_wait(full + 8 * s, ph, a.wait_ns);
-                }
+                if (++s == STAGES) { s = 0; ph ^= 1u; }
+            }
+        } else if (half == 0) {
+            // a wait ran out: the copies in flight land before this memory is given back
+            for (int q = 0; q < STAGES && q < issued; ++q) {
+                if (--s < 0) { s = STAGES - 1; ph ^= 1u; }
+                warp_wait(full + 8 * s, ph, a.wait_ns);
             }
         }
     } else if (warp == 1) {
         // ---------------- MMA issuer (the even CTA of a pair) ----------------
-        if (lane == 0 && half == 0) {
+        if (half == 0) {
             int s = 0;
             uint32_t ph = 0;
             for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
@@ -361,33 +359,37 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
                 const uint32_t sa = smem_u32(smem), sb = sa + S::A_BYTES;
                 const uint64_t a_desc = amn ? sw128_desc_mn(sa, GM_BOX) : sw128_desc(sa);
                 const uint64_t b_desc = bmn ? sw128_desc_mn(sb, GM_BOX) : sw128_desc(sb);
-                if (i >= 2 && !mbar_wait(accempty + 8 * buf, (uint32_t)((i >> 1) & 1) ^ 1u, a.wait_ns)) {
+                if (i >= 2 && !warp_wait(accempty + 8 * buf, (uint32_t)((i >> 1) & 1) ^ 1u, a.wait_ns)) {
                     give_up(12);
                     break;
                 }
                 tc_fence_after();
                 for (int kb = 0; kb < kbs; ++kb) {
-                    if (!mbar_wait(full + 8 * s, ph, a.wait_ns)) {
+                    if (!warp_wait(full + 8 * s, ph, a.wait_ns)) {
                         give_up(13);
                         break;
                     }
                     tc_fence_after();
                     const uint64_t A = a_desc + (uint64_t)((uint32_t)s * (S::STAGE >> 4)), B = b_desc + (uint64_t)((uint32_t)s * (S::STAGE >> 4));
+                    if (elect_one()) {
 #pragma unroll
-                    for (int kk = 0; kk < GM_BK / 16; ++kk)
-                        gm_mma(tmem + (uint32_t)(buf * BN), A + (uint64_t)(kk * da), B + (uint64_t)(kk * db), idesc,
-                               (kb | kk) ? 1u : 0u);
-                    gm_commit(empty + 8 * s, ALL);
+                        for (int kk = 0; kk < GM_BK / 16; ++kk)
+                            gm_mma(tmem + (uint32_t)(buf * BN), A + (uint64_t)(kk * da), B + (uint64_t)(kk * db), idesc,
+                                   (kb | kk) ? 1u : 0u);
+                        gm_commit(empty + 8 * s, ALL);
+                        if (kb + 1 == kbs) gm_commit(accfull + 8 * buf, (uint16_t)(3u << (2 * pair)));
+                    }
+                    __syncwarp();
                     if (++s == STAGES) { s = 0; ph ^= 1u; }
                 }
-                if (aborted()) break;
-                gm_commit(accfull + 8 * buf, (uint16_t)(3u << (2 * pair)));
             }
             if (aborted()) {   // the MMAs issued so far end before TMEM is given back
-                gm_commit(drain, (uint16_t)(1u << rank));
-                mbar_wait(drain, 0, a.wait_ns);
+                if (elect_one()) gm_commit(drain, (uint16_t)(1u << rank));
+                __syncwarp();
+                warp_wait(drain, 0, a.wait_ns);
             }
         }
+        __syncwarp();
     } else {
         // ---------------- epilogue (warps 2..9) ----------------
         const int quarter = warp & 3, side = (warp - 2) >> 2;
@@ -402,7 +404,7 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
         };
-        for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !__any_sync(0xffffffffu, aborted()); ++i) {
+        for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
             const GmTile tl = gm_tile(a, t);
             const GemmProb& pr = a.p[tl.p];
             const int kind = pr.kind, N = pr.N, out = pr.out, buf = i & 1;
@@ -421,7 +423,7 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
                     }
             };
             if (kind == GM_DH) pq_fetch(0);
-            if (!__all_sync(0xffffffffu, mbar_wait(accfull + 8 * buf, (uint32_t)((i >> 1) & 1), a.wait_ns))) {
+            if (!warp_wait(accfull + 8 * buf, (uint32_t)((i >> 1) & 1), a.wait_ns)) {
                 if (lane == 0) give_up(14);
                 break;
             }
@@ -594,7 +596,7 @@ struct GmPlan {
 
 // Clusters that the GPU holds at once (an SM without partners in its group of SMs takes none: the driver says how
 // many fit, 76 pairs or 36 fours of 152 SMs), and the busiest one's clocks: `per` for a stage of 64
-// k-elements and GM_TILE_CLOCKS for a tile.
+// k-elements and `tile` for what of a tile does not run under another's products.
 template <class S>
 cudaError_t gm_fit(int* n) {
     static std::atomic<int> fit[64];   // of a device, asked for once: the answer takes microseconds
@@ -610,7 +612,7 @@ cudaError_t gm_fit(int* n) {
     return e;
 }
 template <class S>
-cudaError_t gm_try(GemmArgs& a, int shape, int per, GmPlan* best) {
+cudaError_t gm_try(GemmArgs& a, int shape, int per, int tile, GmPlan* best) {
     cudaError_t e = smem_optin((const void*)k_mlp_gemm<S>, S::SMEM);
     if (e != cudaSuccess) return e;
     int n = 0;
@@ -619,7 +621,7 @@ cudaError_t gm_try(GemmArgs& a, int shape, int per, GmPlan* best) {
     gm_tiles<S>(a, n);
     const int nc = a.tiles < n ? a.tiles : n;
     // the first problem's tiles go round, then the rest (gm_next)
-    const int64_t ta = (int64_t)a.p[0].kb * per + GM_TILE_CLOCKS, tb = a.nprob > 1 ? (int64_t)a.p[1].kb * per + GM_TILE_CLOCKS : 0;
+    const int64_t ta = (int64_t)a.p[0].kb * per + tile, tb = a.nprob > 1 ? (int64_t)a.p[1].kb * per + tile : 0;
     const int whole = a.na / nc, hi = a.na % nc, rest = a.tiles - a.na - a.head * (nc - hi), r = rest / nc, one = rest % nc;
     const int64_t lo = whole * ta + (a.head + r + (one > hi ? 1 : 0)) * tb;
     const int64_t up = hi ? (whole + 1) * ta + (r + (one ? 1 : 0)) * tb : 0;
@@ -634,9 +636,9 @@ cudaError_t gm_try(GemmArgs& a, int shape, int per, GmPlan* best) {
 
 cudaError_t gm_plan(GemmArgs& a, GmPlan* pl) {
     *pl = {-1, 0, -1};
-    cudaError_t e = gm_try<GmTall>(a, 0, 545, pl);
-    if (e == cudaSuccess) e = gm_try<GmPair>(a, 1, 560, pl);
-    if (e == cudaSuccess) e = gm_try<GmWide>(a, 2, 440, pl);
+    cudaError_t e = gm_try<GmTall>(a, 0, 560, 4000, pl);
+    if (e == cudaSuccess) e = gm_try<GmPair>(a, 1, 565, 4000, pl);
+    if (e == cudaSuccess) e = gm_try<GmWide>(a, 2, 385, 2500, pl);
     return e == cudaSuccess && pl->shape < 0 ? cudaErrorInvalidConfiguration : e;
 }
 

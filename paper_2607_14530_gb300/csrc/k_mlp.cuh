@@ -24,6 +24,18 @@ __device__ __forceinline__ uint32_t map_rank(uint32_t a, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(rank));
     return r;
 }
+// One thread of a converged warp, always the same one.  The loading and the MMA warp walk their loops with all lanes and
+// issue from one: a long loop of a single lane, with the others waiting at the barrier behind it, left
+// that lane without progress in some builds of this kernel.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(p));
+    return p != 0;
+}
+// a bounded wait of a whole warp: true for all lanes or for none
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, uint64_t limit) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, limit));
+}
 // p and q lie in blocks of 32 rows and 8 columns, 24 bytes a row: the upper halves of a block's rows, 16 bytes
 // after 16 bytes, then the third bytes, 8 after 8.  The 32 lanes of an epilogue warp hold 32 rows of the same
 // columns and so write and read 512 and 256 contiguous bytes.

@@ -120,132 +120,138 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
         atomicExch(a.err, code);
         *(volatile int*)&s_abort = 1;
     };
-    auto aborted = [&]() { return *(volatile int*)&s_abort != 0; };
+    auto aborted = [&]() { return __any_sync(0xffffffffu, *(volatile int*)&s_abort != 0) != 0; };   // of a whole warp
     // this CTA's stages of a tile
     auto first_of = [&](const SmPhase& q, int r) { return q.kb * r / SM_S; };
 
     if (warp == 0) {
         // ---------------- TMA producer ----------------
-        if (lane == 0) {
-            int s = 0, issued = 0;
-            uint32_t ph = 0;
-            const uint32_t ring = smem_u32(smem);
-            auto wait_h = [&]() {   // h is whole when every CTA has finished the first product
-                uint64_t t0 = 0;
-                for (uint32_t it = 0; ld_acquire(a.cnt + SM_ARRIVE) < (int)gridDim.x; ++it) {
-                    if ((it & 255u) != 255u) continue;   // reading the timer takes longer than a poll
-                    uint64_t now;
-                    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-                    if (t0 == 0) t0 = now;
-                    if (now - t0 > a.wait_ns || aborted()) {
-                        give_up(22);
-                        break;
-                    }
+        int s = 0, issued = 0;
+        uint32_t ph = 0;
+        const uint32_t ring = smem_u32(smem);
+        auto wait_h = [&]() {   // h is whole when every CTA has finished the first product
+            uint64_t t0 = 0;
+            for (uint32_t it = 0; !__all_sync(0xffffffffu, ld_acquire(a.cnt + SM_ARRIVE) >= (int)gridDim.x); ++it) {
+                if ((it & 255u) != 255u) continue;   // reading the timer takes longer than a poll
+                uint64_t now;
+                asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
+                if (t0 == 0) t0 = now;
+                if (__any_sync(0xffffffffu, now - t0 > a.wait_ns) || aborted()) {
+                    give_up(22);
+                    break;
                 }
-                asm volatile("fence.proxy.async;" ::: "memory");
-            };
-            // a free stage, told what it will receive
-            auto take = [&](int bytes) {
-                if (issued >= STAGES && !mbar_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
-                    give_up(21);
-                    return false;
-                }
-                mbar_expect_tx(full + 8 * s, bytes);
-                return true;
-            };
-            auto next = [&]() {
-                ++issued;
-                if (++s == STAGES) { s = 0; ph ^= 1u; }
-            };
-            {
-                const SmPhase& q = a.ph[0];
-                const int k0 = first_of(q, rank) * 64, k1 = first_of(q, rank + 1) * 64;
-                for (int m = cl; m < q.tiles && k0 < k1 && !aborted(); m += ncl)
-                    for (int k = k0; k < k1 && take(2 * SM_BOX + S::B); k += 64) {
+            }
+            asm volatile("fence.proxy.async;" ::: "memory");
+        };
+        // a free stage, told what it will receive
+        auto take = [&](int bytes) {
+            if (issued >= STAGES && !warp_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
+                give_up(21);
+                return false;
+            }
+            if (elect_one()) mbar_expect_tx(full + 8 * s, bytes);
+            __syncwarp();
+            return true;
+        };
+        auto next = [&]() {
+            __syncwarp();
+            ++issued;
+            if (++s == STAGES) { s = 0; ph ^= 1u; }
+        };
+        {
+            const SmPhase& q = a.ph[0];
+            const int k0 = first_of(q, rank) * 64, k1 = first_of(q, rank + 1) * 64;
+            for (int m = cl; m < q.tiles && k0 < k1 && !aborted(); m += ncl)
+                for (int k = k0; k < k1 && take(2 * SM_BOX + S::B); k += 64) {
+                    if (elect_one()) {
                         const uint32_t st = ring + (uint32_t)s * S::STAGE, bar = full + 8 * s;
                         tma_load_2d(st, &maps.gate, k, m * 64, bar);
                         tma_load_2d(st + SM_BOX, &maps.up, k, m * 64, bar);
                         tma_load_2d(st + 2 * SM_BOX, &maps.x, k, 0, bar);
-                        next();
                     }
-            }
-            if (!aborted()) {
-                const SmPhase& q = a.ph[1];
-                const int k0 = first_of(q, rank) * 128, k1 = first_of(q, rank + 1) * 128;
-                // W_down's boxes, and the tokens' once h is there: until then the ring fills with the weights alone
-                auto weights = [&](int m, int k) {
-                    const uint32_t st = ring + (uint32_t)s * S::STAGE, bar = full + 8 * s;
-                    if (a.down_blocks) {
-                        tma_load_3d(st, &maps.down, 0, m * 64, k / 64, bar);
-                    } else {
-                        tma_load_2d(st, &maps.down, k, m * 64, bar);
-                        tma_load_2d(st + SM_BOX, &maps.down, k + 64, m * 64, bar);
-                    }
-                };
-                auto tokens = [&](int at, int k) {
-                    const uint32_t st = ring + (uint32_t)at * S::STAGE + 2 * SM_BOX, bar = full + 8 * at;
-                    if (a.down_blocks) {
-                        tma_load_3d(st, &maps.h, 0, 0, k / 64, bar);
-                    } else {
-                        tma_load_2d(st, &maps.h, k, 0, bar);
-                        tma_load_2d(st + S::B, &maps.h, k + 64, 0, bar);
-                    }
-                };
-                const int s0 = s;
-                int ahead = 0, m = cl, k = k0;
-                for (; m < q.tiles && k0 < k1 && ahead < STAGES; ++ahead) {
-                    if (!take(2 * SM_BOX + 2 * S::B)) break;
-                    weights(m, k);
                     next();
-                    if ((k += 128) == k1) { k = k0; m += ncl; }
                 }
-                if (ahead > 0) {
-                    if (!aborted()) wait_h();
-                    // (given up: loaded all the same, so that every stage begun is complete)
-                    for (int j = 0, at = s0, kt = k0; j < ahead; ++j) {
-                        tokens(at, kt);
-                        if (++at == STAGES) at = 0;
-                        if ((kt += 128) == k1) kt = k0;
-                    }
+        }
+        if (!aborted()) {
+            const SmPhase& q = a.ph[1];
+            const int k0 = first_of(q, rank) * 128, k1 = first_of(q, rank + 1) * 128;
+            // W_down's boxes, and the tokens' once h is there: until then the ring fills with the weights alone
+            auto weights = [&](int m, int k) {
+                const uint32_t st = ring + (uint32_t)s * S::STAGE, bar = full + 8 * s;
+                if (!elect_one()) return;
+                if (a.down_blocks) {
+                    tma_load_3d(st, &maps.down, 0, m * 64, k / 64, bar);
+                } else {
+                    tma_load_2d(st, &maps.down, k, m * 64, bar);
+                    tma_load_2d(st + SM_BOX, &maps.down, k + 64, m * 64, bar);
                 }
-                for (; m < q.tiles && k0 < k1 && !aborted(); m += ncl, k = k0)
-                    for (; k < k1 && take(2 * SM_BOX + 2 * S::B); k += 128) {
-                        weights(m, k);
-                        tokens(s, k);
-                        next();
-                    }
+            };
+            auto tokens = [&](int at, int k) {
+                const uint32_t st = ring + (uint32_t)at * S::STAGE + 2 * SM_BOX, bar = full + 8 * at;
+                if (!elect_one()) return;
+                if (a.down_blocks) {
+                    tma_load_3d(st, &maps.h, 0, 0, k / 64, bar);
+                } else {
+                    tma_load_2d(st, &maps.h, k, 0, bar);
+                    tma_load_2d(st + S::B, &maps.h, k + 64, 0, bar);
+                }
+            };
+            const int s0 = s;
+            int ahead = 0, m = cl, k = k0;
+            for (; m < q.tiles && k0 < k1 && ahead < STAGES; ++ahead) {
+                if (!take(2 * SM_BOX + 2 * S::B)) break;
+                weights(m, k);
+                next();
+                if ((k += 128) == k1) { k = k0; m += ncl; }
             }
-            if (aborted()) {
-                // a wait ran out: the copies in flight land before this memory is given back
-                for (int q = 0; q < STAGES && q < issued; ++q) {
-                    if (--s < 0) { s = STAGES - 1; ph ^= 1u; }
-                    mbar_wait(full + 8 * s, ph, a.wait_ns);
+            if (ahead > 0) {
+                if (!aborted()) wait_h();
+                // (given up: loaded all the same, so that every stage begun is complete)
+                for (int j = 0, at = s0, kt = k0; j < ahead; ++j) {
+                    tokens(at, kt);
+                    __syncwarp();
+                    if (++at == STAGES) at = 0;
+                    if ((kt += 128) == k1) kt = k0;
                 }
+            }
+            for (; m < q.tiles && k0 < k1 && !aborted(); m += ncl, k = k0)
+                for (; k < k1 && take(2 * SM_BOX + 2 * S::B); k += 128) {
+                    weights(m, k);
+                    __syncwarp();
+                    tokens(s, k);
+                    next();
+                }
+        }
+        if (aborted()) {
+            // a wait ran out: the copies in flight land before this memory is given back
+            for (int q = 0; q < STAGES && q < issued; ++q) {
+                if (--s < 0) { s = STAGES - 1; ph ^= 1u; }
+                warp_wait(full + 8 * s, ph, a.wait_ns);
             }
         }
     } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
-        if (lane == 0) {
-            const uint32_t idesc = idesc_bf16(128, NT);
-            int s = 0, seg = 0;
-            uint32_t ph = 0;
-            for (int f = 0; f < 2 && !aborted(); ++f) {
-                const SmPhase& q = a.ph[f];
-                const int n = first_of(q, rank + 1) - first_of(q, rank);
-                for (int m = cl; m < q.tiles && n > 0 && !aborted(); m += ncl, ++seg) {
-                    const uint32_t d = tmem + (uint32_t)((seg & 1) * 2 * NT);
-                    if (seg >= 2 && !mbar_wait(accempty + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1) ^ 1u, a.wait_ns)) {
-                        give_up(23);
+        const uint32_t idesc = idesc_bf16(128, NT);
+        int s = 0, seg = 0;
+        uint32_t ph = 0;
+        for (int f = 0; f < 2 && !aborted(); ++f) {
+            const SmPhase& q = a.ph[f];
+            const int n = first_of(q, rank + 1) - first_of(q, rank);
+            for (int m = cl; m < q.tiles && n > 0 && !aborted(); m += ncl, ++seg) {
+                const uint32_t d = tmem + (uint32_t)((seg & 1) * 2 * NT);
+                if (seg >= 2 && !warp_wait(accempty + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1) ^ 1u, a.wait_ns)) {
+                    give_up(23);
+                    break;
+                }
+                tc_fence_after();
+                for (int kb = 0; kb < n; ++kb) {
+                    if (!warp_wait(full + 8 * s, ph, a.wait_ns)) {
+                        give_up(24);
                         break;
                     }
                     tc_fence_after();
-                    for (int kb = 0; kb < n; ++kb) {
-                        if (!mbar_wait(full + 8 * s, ph, a.wait_ns)) {
-                            give_up(24);
-                            break;
-                        }
-                        tc_fence_after();
-                        const uint32_t sa = smem_u32(smem + s * S::STAGE), sb = sa + 2 * SM_BOX;
+                    const uint32_t sa = smem_u32(smem + s * S::STAGE), sb = sa + 2 * SM_BOX;
+                    if (elect_one()) {
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk) {
                             const uint32_t on = kb == 0 && kk == 0 ? 0u : 1u;
@@ -253,16 +259,17 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
                             if (f) mma_bf16(d + NT, sw128_desc(sa + kk * 32), sw128_desc(sb + S::B + kk * 32), idesc, on);
                         }
                         mma_commit(empty + 8 * s);
-                        if (++s == STAGES) { s = 0; ph ^= 1u; }
+                        if (kb + 1 == n) mma_commit(accfull + 8 * (seg & 1));
                     }
-                    if (aborted()) break;
-                    mma_commit(accfull + 8 * (seg & 1));
+                    __syncwarp();
+                    if (++s == STAGES) { s = 0; ph ^= 1u; }
                 }
             }
-            // all MMAs are done before the ring and TMEM are given back
-            mma_commit(drain);
-            if (!mbar_wait(drain, 0, a.wait_ns)) give_up(25);
         }
+        // all MMAs are done before the ring and TMEM are given back
+        if (elect_one()) mma_commit(drain);
+        __syncwarp();
+        if (!warp_wait(drain, 0, a.wait_ns)) give_up(25);
     } else {
         // ---------------- epilogue (warps 2..5) ----------------
         const int quarter = warp & 3;
@@ -276,7 +283,7 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
         auto agree = [&](bool mine) {
             int all;
             asm volatile("{\n .reg .pred p, q;\n setp.ne.s32 p, %1, 0;\n bar.red.and.pred q, 2, 128, p;\n selp.s32 %0, 1, 0, q;\n}\n"
-                         : "=r"(all) : "r"(mine && !aborted() ? 1 : 0) : "memory");
+                         : "=r"(all) : "r"(mine && *(volatile int*)&s_abort == 0 ? 1 : 0) : "memory");
             return all != 0;
         };
         for (int f = 0; f < 2 && ok; ++f) {
@@ -286,7 +293,7 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
             for (int r = 0; r < SM_S; ++r) parts += first_of(q, r) < first_of(q, r + 1) ? 1 : 0;
             for (int m = cl; m < q.tiles && ok; m += ncl) {
                 const uint32_t d = tmem + (uint32_t)((seg & 1) * 2 * NT + (f ? side * NT : 0)) + ((uint32_t)(quarter * 32) << 16);
-                const bool done = !part || mbar_wait(accfull + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1), a.wait_ns);
+                const bool done = !part || warp_wait(accfull + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1), a.wait_ns);
                 if (!done) give_up(26);
                 if (!(ok = agree(done))) break;
                 tc_fence_after();
@@ -310,7 +317,7 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
                         }
                     }
                     if (threadIdx.x == 64) mbar_expect_tx(recv + 8 * b, (uint32_t)(parts * nt * 2 * 16 * 4));
-                    const bool got = mbar_wait(recv + 8 * b, (uint32_t)((round >> 1) & 1), a.wait_ns);
+                    const bool got = warp_wait(recv + 8 * b, (uint32_t)((round >> 1) & 1), a.wait_ns);
                     if (!got) give_up(27);
                     const float* in = reinterpret_cast<const float*>(recv_mem + b * S::RECV);
                     for (int i = 2 * quarter + (lane >> 4); i < nt && got; i += 8) {

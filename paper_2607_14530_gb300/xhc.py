@@ -769,9 +769,9 @@ def clip_grads(grads, max_norm: float, scale: float = 1.0, eps: float = 1e-6, ou
 
     def checked(ts, what):
         """The pointers, sizes and types of a list of tensors."""
-        for q, t in enumerate(ts):
-            if t.get_device() != device or not t.is_contiguous():
-                raise XhcError(f"{what} {q} must be a contiguous CUDA tensor on the current device")
+        if [t.get_device() for t in ts].count(device) != len(ts) or False in [t.is_contiguous() for t in ts]:
+            q = [t.get_device() == device and t.is_contiguous() for t in ts].index(False)
+            raise XhcError(f"{what} {q} must be a contiguous CUDA tensor on the current device")
         types = [t.dtype for t in ts]
         if not _CLIP_TYPES.issuperset(types):
             raise XhcError(f"every {what} must be an fp32 or bf16 tensor")
