@@ -323,7 +323,7 @@ typedef enum { XHC_F32 = 0, XHC_BF16 = 1 } xhc_dtype;
  * captured graphs that may run at once, need workspaces of their own.  x and y (dy and dx) may not overlap.
  * Limits: C % 8 == 0, F % 8 == 0, 8 <= C <= 16384, 8 <= F <= 65536, 1 <= T <= 2^24, pointers 16-byte
  * aligned; every result is the same, to the bit, from run to run, and y of
- * up to 16 tokens (64 where C F >= 2^21) also whatever the other tokens and their number. */
+ * up to 64 tokens (128 where C F >= 2^23) also whatever the other tokens and their number. */
 #define XHC_MLP_HEADER_BYTES 256
 typedef enum { XHC_ACT_SILU = 0, XHC_ACT_GELU = 1, XHC_ACT_RELU = 2 } xhc_act;   /* GELU: x Phi(x) */
 typedef struct {

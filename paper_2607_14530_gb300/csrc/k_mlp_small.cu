@@ -1,10 +1,10 @@
 // The feed-forward block's forward for few tokens (a decode step), in one launch:
 //   h = act(x W_gate^T) * (x W_up^T), then y = h W_down^T
 // It is bound by reading the weights once, 6 C F bytes.  The weights are the MMA's A operand (M = 128), the tokens its
-// N of 16 to 64: outputs transposed.  A tile is 64 outputs: of the first product 64 rows of W_gate above 64 of W_up;
+// N of 16 to 128: outputs transposed.  A tile is 64 outputs: of the first product 64 rows of W_gate above 64 of W_up;
 // of the second the same 64 rows of W_down at two neighbouring k-steps, each multiplied with both steps'
 // tokens, of which one half of the rows is used.  (Tiles of 128 outputs: 16 of them at C = 2048 left most SMs
-// without work in the second product, 26 us a call for 24 tokens of F = 5632.)
+// without work in the second product, 26 us a call for 24 tokens of F = 5632, now 22.)
 // A cluster of four CTAs takes a tile, a quarter of its k-range each, through rings of 192 to 200 KB that keep
 // the memory busy.  The four partial sums meet in shared memory: the lanes that hold rows 16 j .. 16 j + 15 send
 // them to CTA j (st.async, which counts on j's barrier), and CTA j adds the four in order and finishes these
@@ -30,7 +30,7 @@ constexpr int SM_ARRIVE = 0, SM_LEAVE = 1;   // counters
 template <int NT>
 struct SmShape {
     static constexpr int B = NT * 64 * 2, STAGE = 2 * SM_BOX + 2 * B;
-    static constexpr int STAGES = NT == 16 ? 10 : NT == 32 ? 8 : 6;
+    static constexpr int STAGES = NT == 16 ? 10 : NT == 32 ? 8 : NT == 64 ? 6 : 4;
     static constexpr int RT = NT < 32 ? NT : 32;            // tokens exchanged at a time
     static constexpr int PART = 2 * RT * 16;                // floats of a CTA's part: [half][token][row]
     static constexpr int RECV = SM_S * PART * 4;
@@ -413,10 +413,10 @@ cudaError_t sm_launch_act(int act, const SmMaps& maps, const SmArgs& a, cudaStre
 
 }  // namespace
 
-// Up to 64 tokens where the weights are 12 MB or more, 16 where they are less: us a call here / with the tiles
-// of k_mlp.cu, C = 4096, F = 11008: 80 / 104 at 64 tokens, 105 / 104 at 128; C = 1024, F = 2816: 17.6 / 29.7 at 1, 25.4 /
-// 25.3 at 64; C = 264, F = 712: 13.4 / 13.3 at 1, 14.4 / 13.5 at 16, 21.3 / 13.8 at 64.
-bool mlp_small(int64_t T, int C, int F) { return T <= ((int64_t)C * F >= (int64_t)1 << 21 ? 64 : 16); }
+// Up to 64 tokens, 128 where the weights are 48 MB or more: us a call here / with the tiles of k_mlp.cu, captured,
+// C = 4096, F = 11008: 51 / 117 at 1 token, 58 / 86 at 64, 72 / 88 at 128; C = 2048, F = 5632: 21 / 40 at 1, 31 / 38 at 65, 40 / 39
+// at 128; C = 1024, F = 2816: 13 / 27 at 1, 20 / 21 at 64, 22 / 21 at 65; C = 264, F = 712: 8.5 / 12.3 at 1, 13 / 13 at 64.
+bool mlp_small(int64_t T, int C, int F) { return T <= ((int64_t)C * F >= (int64_t)1 << 23 ? 128 : 64); }
 
 cudaError_t launch_mlp_small(int T, int C, int F, int act, const uint16_t* x, const uint16_t* Wg, const uint16_t* Wu,
                              const uint16_t* Wd, uint16_t* h, void* pq, uint16_t* y, int* cnt, int* err, cudaStream_t st) {
@@ -433,7 +433,7 @@ cudaError_t launch_mlp_small(int T, int C, int F, int act, const uint16_t* x, co
     a.q_off = (int64_t)mlp_pq_bytes(T, F);
     a.wait_ns = debug_wait_ns();
     a.err = err;
-    const int NT = T <= 16 ? 16 : T <= 32 ? 32 : 64;
+    const int NT = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128;
     SmMaps m;
     if (!make_map_box(&m.gate, Wg, C, F, 64, 64) || !make_map_box(&m.up, Wu, C, F, 64, 64) ||
         !make_map_box(&m.x, x, C, T, 64, NT))
@@ -444,7 +444,8 @@ cudaError_t launch_mlp_small(int T, int C, int F, int act, const uint16_t* x, co
         return cudaErrorInvalidValue;
     if (NT == 16) return sm_launch_act<16>(act, m, a, st);
     if (NT == 32) return sm_launch_act<32>(act, m, a, st);
-    return sm_launch_act<64>(act, m, a, st);
+    if (NT == 64) return sm_launch_act<64>(act, m, a, st);
+    return sm_launch_act<128>(act, m, a, st);
 }
 
 }  // namespace xhc

@@ -47,7 +47,8 @@ SHAPES = [(1, 8, 8), (1, 264, 712), (2, 64, 128), (3, 72, 136), (7, 512, 1032), 
           (32, 128, 64), (33, 128, 72), (64, 520, 1024), (65, 256, 384), (100, 2056, 264), (127, 512, 512), (128, 512, 512),
           (129, 264, 712), (255, 384, 1000), (256, 1024, 256), (257, 256, 2048), (333, 264, 712), (700, 512, 1544),
           (1029, 2048, 1384), (2500, 1024, 2816), (1, 1024, 2816), (16, 2056, 1384), (17, 4096, 1032), (40, 1024, 2816), (64, 1544, 2056),
-          (65, 1024, 2816), (4099, 512, 1032), (1200, 4096, 264)]
+          (65, 1024, 2816), (4099, 512, 1032), (1200, 4096, 264), (64, 264, 712), (48, 136, 200),
+          (128, 2048, 4160), (97, 2056, 4096)]
 
 
 @pytest.mark.parametrize("T,C,F", SHAPES)
@@ -99,14 +100,14 @@ def test_fp32_gradients_written_and_accumulated(T, C, F):
         assert torch.equal(b[n], got[n].to(BF)), n
 
 
-@pytest.mark.parametrize("C,F", [(264, 712), (512, 1544), (4096, 1024)])
+@pytest.mark.parametrize("C,F", [(264, 712), (512, 1544), (4096, 1024), (2048, 4160)])
 def test_few_tokens_keep_their_bits_in_any_batch(C, F):
-    most = 64 if C * F >= 2 ** 21 else 16
+    most = 128 if C * F >= 2 ** 23 else 64
     x, P, _ = inputs(most, C, F, seed=2)
     x, op = x.cuda(), Mlp(C, F)
     ws = poisoned(op, most)[1]
     want = op.forward(P, x, ws)
-    for T in (1, 2, 8, 15, 16, 17, 32, 33, 63):
+    for T in (1, 2, 8, 15, 16, 17, 32, 33, 63, 64, 65, 96, 127):
         if T <= most:
             ws = poisoned(op, T)[1]
             assert torch.equal(op.forward(P, x[:T], ws), want[:T]), T
