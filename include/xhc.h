@@ -317,14 +317,12 @@ typedef enum { XHC_F32 = 0, XHC_BF16 = 1 } xhc_dtype;
  * xhc_mlp_bwd writes dx [T, C] bf16 and the weight gradients, shaped like the weights, in fp32
  *   (XHC_F32; accumulate = 1 adds to what is there) or rounded once to bf16 (XHC_BF16; accumulate
  *   has to be 0, else XHC_ERR_UNSUPPORTED).  x, W and `saved` are the forward's.
- * `workspace` (xhc_mlp_workspace_bytes) is scratch of one call; a fresh one needs its first
- * XHC_MLP_HEADER_BYTES zeroed (its device error word, xhc_workspace_error, and counters that every call
- * leaves at zero; after XHC_ERR_TIMEOUT they have to be zeroed again).  Two calls in flight on different streams, or in two
+ * `workspace` (xhc_mlp_workspace_bytes) is scratch of one call; a fresh one needs its first 256 bytes zeroed
+ * (its device error word, xhc_workspace_error).  Two calls in flight on different streams, or in two
  * captured graphs that may run at once, need workspaces of their own.  x and y (dy and dx) may not overlap.
  * Limits: C % 8 == 0, F % 8 == 0, 8 <= C <= 16384, 8 <= F <= 65536, 1 <= T <= 2^24, pointers 16-byte
  * aligned; every result is the same, to the bit, from run to run, and y of
  * up to 64 tokens (128 where C F >= 2^23) also whatever the other tokens and their number. */
-#define XHC_MLP_HEADER_BYTES 256
 typedef enum { XHC_ACT_SILU = 0, XHC_ACT_GELU = 1, XHC_ACT_RELU = 2 } xhc_act;   /* GELU: x Phi(x) */
 typedef struct {
     int C;      /* hidden size                    */

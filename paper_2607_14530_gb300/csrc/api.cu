@@ -1083,7 +1083,7 @@ namespace {
 // `saved` and `workspace` of the gated feed-forward block
 struct MlpLayout {
     size_t h, pq, saved_total;                // saved: bf16 [T][F], then p and q (mlp_pq_bytes each)
-    size_t err, cnt, hs, dg, du, ws_total;    // workspace: h of a forward without `saved` where dg is
+    size_t err, hs, dg, du, ws_total;         // workspace: h of a forward without `saved` where dg is
 };
 
 MlpLayout mlp_layout(int64_t T, int F) {
@@ -1093,9 +1093,7 @@ MlpLayout mlp_layout(int64_t T, int F) {
     L.pq = tf;
     L.saved_total = al(tf + 2 * mlp_pq_bytes(T, F));
     L.err = 0;
-    L.cnt = 64;
-    static_assert(64 + MLP_COUNTERS * 4 <= XHC_MLP_HEADER_BYTES, "counters in the header");
-    L.hs = L.dg = XHC_MLP_HEADER_BYTES;
+    L.hs = L.dg = 256;
     L.du = L.dg + tf;
     L.ws_total = L.du + tf;
     return L;
@@ -1150,8 +1148,9 @@ xhc_status xhc_mlp_fwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
     uint16_t* h = (uint16_t*)(sv ? sv + L.h : ws + L.hs);
     int* err = (int*)(ws + L.err);
     if (mlp_small(T, C, F)) {
-        XHC_K("mlp_small", st, launch_mlp_small(T32, C, F, cfg->act, x, W->gate, W->up, W->down, h, sv ? sv + L.pq : nullptr, y,
-                                                (int*)(ws + L.cnt), err, st));
+        XHC_K("mlp_small_gate", st, launch_mlp_small_gate(T32, C, F, cfg->act, x, W->gate, W->up, h, sv ? sv + L.pq : nullptr,
+                                                          err, st));
+        XHC_K("mlp_small_down", st, launch_mlp_small_down(T32, C, F, h, W->down, y, err, st));
         return XHC_OK;
     }
     XHC_K("mlp_gate", st, launch_mlp_gate(T32, C, F, cfg->act, x, W->gate, W->up, h,

@@ -1,19 +1,18 @@
-// The feed-forward block's forward for few tokens (a decode step), in one launch:
+// The feed-forward block's forward for few tokens (a decode step), in two launches:
 //   h = act(x W_gate^T) * (x W_up^T), then y = h W_down^T
 // It is bound by reading the weights once, 6 C F bytes.  The weights are the MMA's A operand (M = 128), the tokens its
 // N of 16 to 128: outputs transposed.  A tile is 64 outputs: of the first product 64 rows of W_gate above 64 of W_up;
 // of the second the same 64 rows of W_down at two neighbouring k-steps, each multiplied with both steps'
 // tokens, of which one half of the rows is used.  (Tiles of 128 outputs: 16 of them at C = 2048 left most SMs
-// without work in the second product, 26 us a call for 24 tokens of F = 5632, now 22.)
-// A cluster of four CTAs takes a tile, a quarter of its k-range each, through rings of 192 to 200 KB that keep
+// without work in the second product.)
+// A cluster of four CTAs takes a tile, a quarter of its k-range each, through rings of about 190 KB that keep
 // the memory busy.  The four partial sums meet in shared memory: the lanes that hold rows 16 j .. 16 j + 15 send
 // them to CTA j (st.async, which counts on j's barrier), and CTA j adds the four in order and finishes these
 // rows.  (Equal shares of the stream for every SM with the parts left in L2 and waited for by
 // counters took 59 us at C = 4096, F = 11008: every exchange is four trips through L2.)
 // The cut depends on C and F alone: a token's bits do not depend on the other tokens or on their number.
-// The second product needs all of h: the CTAs (one an SM, launched cooperatively, so all are there) meet at a
-// counter.  Loads of W_down do not need h and fill the ring before that wait, so the stream of weights
-// hardly stops between the products.
+// The second launch is placed as the first one's CTAs end, and fills its rings with W_down, which the first one does not
+// write, before it waits for h.
 #include <atomic>
 
 #include "k_mlp.cuh"
@@ -25,56 +24,51 @@ namespace {
 constexpr int SM_NT = 192;                   // warp 0 TMA, warp 1 MMA, warps 2..5 epilogue
 constexpr int SM_S = 4;                      // CTAs of a cluster
 constexpr int SM_BOX = 64 * 64 * 2;          // a box of 64 weight rows and 64 k-elements; two a stage
-constexpr int SM_ARRIVE = 0, SM_LEAVE = 1;   // counters
 
-template <int NT>
+// GATE: the first product
+template <int NT, bool GATE>
 struct SmShape {
-    static constexpr int B = NT * 64 * 2, STAGE = 2 * SM_BOX + 2 * B;
-    static constexpr int STAGES = NT == 16 ? 10 : NT == 32 ? 8 : NT == 64 ? 6 : 4;
+    static constexpr int B = NT * 64 * 2, STEPS = GATE ? 1 : 2;   // k-steps of 64 a stage
+    static constexpr int STAGE = 2 * SM_BOX + STEPS * B;
     static constexpr int RT = NT < 32 ? NT : 32;            // tokens exchanged at a time
     static constexpr int PART = 2 * RT * 16;                // floats of a CTA's part: [half][token][row]
     static constexpr int RECV = SM_S * PART * 4;
+    static constexpr int STAGES = (224 * 1024 - 2 * RECV) / STAGE < 10 ? (224 * 1024 - 2 * RECV) / STAGE : 10;
     static constexpr int SMEM = STAGES * STAGE + 2 * RECV + (2 * STAGES + 7) * 8 + 16 + 1024;
     static constexpr uint32_t COLS = 4 * NT;                // two accumulators of two times NT columns
 };
 
-// One of the two products: `tiles` weight tiles of `kb` stages; cluster c takes tiles c, c + clusters, ..., its CTA r
-// stages [kb r / 4, kb (r + 1) / 4) of each.
-struct SmPhase {
-    int kb, tiles;
-};
 struct SmMaps {
-    CUtensorMap gate, up, down, x, h;
+    CUtensorMap w, up, tok;   // W_gate, W_up and x, or W_down and h
 };
 struct SmArgs {
-    int T, C, F;
-    int down_blocks;       // W_down and h in boxes of two k-steps (64 divides F)
-    SmPhase ph[2];
-    int* cnt;              // counters, zero between launches
-    uint16_t *h, *y;
+    int T, out;            // tokens, output columns
+    int kb, tiles;         // stages of a tile; cluster c takes tiles c, c + clusters, ..., its CTA r stages
+                           // [kb r / 4, kb (r + 1) / 4) of each
+    int blocks;            // the second product's boxes hold two k-steps (64 divides F)
+    uint16_t* y;           // h, or y
     unsigned char* pq;     // p, then q (null: not kept)
     int64_t q_off;
     uint64_t wait_ns;
     int* err;
 };
 
-__device__ __forceinline__ int ld_acquire(const int* p) {
-    int v;
-    asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
-    return v;
-}
-// after a barrier: what all its threads wrote before is seen by whoever sees the sum
-__device__ __forceinline__ void add_release(int* p) {
-    asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p) : "memory");
-}
 // into the shared memory of a CTA of the cluster, counted in bytes on its barrier
 __device__ __forceinline__ void send(uint32_t to, float a, uint32_t bar) {
     asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(to), "r"(__float_as_uint(a)), "r"(bar) : "memory");
 }
-template <int NT, int ACT>
+
+// The second launch reads W_down before it waits for the first.  It may: it is placed only when every CTA of the first
+// has called this, and that is after the first's own wait, so all that came before the two in the stream is done.
+__device__ __forceinline__ void late_pdl_entry() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+template <int NT, int ACT, bool GATE>
 __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ SmMaps maps, const __grid_constant__ SmArgs a) {
-    using S = SmShape<NT>;
-    constexpr int STAGES = S::STAGES, RT = S::RT;
+    using S = SmShape<NT, GATE>;
+    constexpr int STAGES = S::STAGES, RT = S::RT, STEP = 64 * S::STEPS;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     unsigned char* recv_mem = smem + STAGES * S::STAGE;
@@ -82,7 +76,7 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, accfull = empty + 8 * STAGES, accempty = accfull + 16,
                    recv = accempty + 16, drain = recv + 16;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 7);
-    __shared__ int s_abort, s_last;
+    __shared__ int s_abort;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)cluster_rank(), cl = blockIdx.x / SM_S, ncl = gridDim.x / SM_S;
@@ -105,8 +99,8 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(S::COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
-    if (warp == 2 && lane < 5) {
-        const CUtensorMap* m = lane == 0 ? &maps.gate : lane == 1 ? &maps.up : lane == 2 ? &maps.x : lane == 3 ? &maps.down : &maps.h;
+    if (warp == 2 && lane < 3) {
+        const CUtensorMap* m = lane == 0 ? &maps.w : lane == 1 ? &maps.up : &maps.tok;
         asm volatile("prefetch.tensormap [%0];" ::"l"((uint64_t)m) : "memory");
     }
     tc_fence_before();
@@ -114,114 +108,87 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
     cluster_sync();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    pdl_entry();
+    if (GATE) late_pdl_entry();
+    else if (warp != 0) pdl_entry();   // the loading warp: below
 
     auto give_up = [&](int code) {
         atomicExch(a.err, code);
         *(volatile int*)&s_abort = 1;
     };
     auto aborted = [&]() { return __any_sync(0xffffffffu, *(volatile int*)&s_abort != 0) != 0; };   // of a whole warp
-    // this CTA's stages of a tile
-    auto first_of = [&](const SmPhase& q, int r) { return q.kb * r / SM_S; };
+    const int kb0 = a.kb * rank / SM_S, kb1 = a.kb * (rank + 1) / SM_S;   // this CTA's stages of a tile
 
     if (warp == 0) {
         // ---------------- TMA producer ----------------
         int s = 0, issued = 0;
         uint32_t ph = 0;
         const uint32_t ring = smem_u32(smem);
-        auto wait_h = [&]() {   // h is whole when every CTA has finished the first product
-            uint64_t t0 = 0;
-            for (uint32_t it = 0; !__all_sync(0xffffffffu, ld_acquire(a.cnt + SM_ARRIVE) >= (int)gridDim.x); ++it) {
-                if ((it & 255u) != 255u) continue;   // reading the timer takes longer than a poll
-                uint64_t now;
-                asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(now));
-                if (t0 == 0) t0 = now;
-                if (__any_sync(0xffffffffu, now - t0 > a.wait_ns) || aborted()) {
-                    give_up(22);
-                    break;
-                }
-            }
-            asm volatile("fence.proxy.async;" ::: "memory");
-        };
+        const int k0 = kb0 * STEP, k1 = kb1 * STEP;
         // a free stage, told what it will receive
-        auto take = [&](int bytes) {
+        auto take = [&]() {
             if (issued >= STAGES && !warp_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
                 give_up(21);
                 return false;
             }
-            if (elect_one()) mbar_expect_tx(full + 8 * s, bytes);
+            if (elect_one()) mbar_expect_tx(full + 8 * s, S::STAGE);
             __syncwarp();
             return true;
         };
         auto next = [&]() {
-            __syncwarp();
             ++issued;
             if (++s == STAGES) { s = 0; ph ^= 1u; }
         };
-        {
-            const SmPhase& q = a.ph[0];
-            const int k0 = first_of(q, rank) * 64, k1 = first_of(q, rank + 1) * 64;
-            for (int m = cl; m < q.tiles && k0 < k1 && !aborted(); m += ncl)
-                for (int k = k0; k < k1 && take(2 * SM_BOX + S::B); k += 64) {
-                    if (elect_one()) {
-                        const uint32_t st = ring + (uint32_t)s * S::STAGE, bar = full + 8 * s;
-                        tma_load_2d(st, &maps.gate, k, m * 64, bar);
-                        tma_load_2d(st + SM_BOX, &maps.up, k, m * 64, bar);
-                        tma_load_2d(st + 2 * SM_BOX, &maps.x, k, 0, bar);
-                    }
-                    next();
-                }
-        }
-        if (!aborted()) {
-            const SmPhase& q = a.ph[1];
-            const int k0 = first_of(q, rank) * 128, k1 = first_of(q, rank + 1) * 128;
-            // W_down's boxes, and the tokens' once h is there: until then the ring fills with the weights alone
-            auto weights = [&](int m, int k) {
+        auto weights = [&](int m, int k) {
+            if (elect_one()) {
                 const uint32_t st = ring + (uint32_t)s * S::STAGE, bar = full + 8 * s;
-                if (!elect_one()) return;
-                if (a.down_blocks) {
-                    tma_load_3d(st, &maps.down, 0, m * 64, k / 64, bar);
+                if (GATE) {
+                    tma_load_2d(st, &maps.w, k, m * 64, bar);
+                    tma_load_2d(st + SM_BOX, &maps.up, k, m * 64, bar);
+                } else if (a.blocks) {
+                    tma_load_3d(st, &maps.w, 0, m * 64, k / 64, bar);
                 } else {
-                    tma_load_2d(st, &maps.down, k, m * 64, bar);
-                    tma_load_2d(st + SM_BOX, &maps.down, k + 64, m * 64, bar);
+                    tma_load_2d(st, &maps.w, k, m * 64, bar);
+                    tma_load_2d(st + SM_BOX, &maps.w, k + 64, m * 64, bar);
                 }
-            };
-            auto tokens = [&](int at, int k) {
+            }
+            __syncwarp();
+        };
+        auto tokens = [&](int at, int k) {
+            if (elect_one()) {
                 const uint32_t st = ring + (uint32_t)at * S::STAGE + 2 * SM_BOX, bar = full + 8 * at;
-                if (!elect_one()) return;
-                if (a.down_blocks) {
-                    tma_load_3d(st, &maps.h, 0, 0, k / 64, bar);
+                if (GATE) {
+                    tma_load_2d(st, &maps.tok, k, 0, bar);
+                } else if (a.blocks) {
+                    tma_load_3d(st, &maps.tok, 0, 0, k / 64, bar);
                 } else {
-                    tma_load_2d(st, &maps.h, k, 0, bar);
-                    tma_load_2d(st + S::B, &maps.h, k + 64, 0, bar);
+                    tma_load_2d(st, &maps.tok, k, 0, bar);
+                    tma_load_2d(st + S::B, &maps.tok, k + 64, 0, bar);
                 }
-            };
-            const int s0 = s;
-            int ahead = 0, m = cl, k = k0;
-            for (; m < q.tiles && k0 < k1 && ahead < STAGES; ++ahead) {
-                if (!take(2 * SM_BOX + 2 * S::B)) break;
+            }
+            __syncwarp();
+        };
+        int m = cl, k = k0;
+        if (!GATE) {
+            // the ring filled with the weights alone, then h's part of these stages
+            int ahead = 0;
+            for (; m < a.tiles && k0 < k1 && ahead < STAGES; ++ahead) {
+                take();   // (never used before: nothing to wait for)
                 weights(m, k);
                 next();
-                if ((k += 128) == k1) { k = k0; m += ncl; }
+                if ((k += STEP) == k1) { k = k0; m += ncl; }
             }
-            if (ahead > 0) {
-                if (!aborted()) wait_h();
-                // (given up: loaded all the same, so that every stage begun is complete)
-                for (int j = 0, at = s0, kt = k0; j < ahead; ++j) {
-                    tokens(at, kt);
-                    __syncwarp();
-                    if (++at == STAGES) at = 0;
-                    if ((kt += 128) == k1) kt = k0;
-                }
+            pdl_entry();
+            for (int j = 0, kt = k0; j < ahead; ++j) {
+                tokens(j, kt);
+                if ((kt += STEP) == k1) kt = k0;
             }
-            for (; m < q.tiles && k0 < k1 && !aborted(); m += ncl, k = k0)
-                for (; k < k1 && take(2 * SM_BOX + 2 * S::B); k += 128) {
-                    weights(m, k);
-                    __syncwarp();
-                    tokens(s, k);
-                    next();
-                }
         }
+        for (; m < a.tiles && k0 < k1 && !aborted(); m += ncl, k = k0)
+            for (; k < k1 && take(); k += STEP) {
+                weights(m, k);
+                tokens(s, k);
+                next();
+            }
         if (aborted()) {
             // a wait ran out: the copies in flight land before this memory is given back
             for (int q = 0; q < STAGES && q < issued; ++q) {
@@ -232,38 +199,35 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
     } else if (warp == 1) {
         // ---------------- MMA issuer ----------------
         const uint32_t idesc = idesc_bf16(128, NT);
+        const int n = kb1 - kb0;
         int s = 0, seg = 0;
         uint32_t ph = 0;
-        for (int f = 0; f < 2 && !aborted(); ++f) {
-            const SmPhase& q = a.ph[f];
-            const int n = first_of(q, rank + 1) - first_of(q, rank);
-            for (int m = cl; m < q.tiles && n > 0 && !aborted(); m += ncl, ++seg) {
-                const uint32_t d = tmem + (uint32_t)((seg & 1) * 2 * NT);
-                if (seg >= 2 && !warp_wait(accempty + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1) ^ 1u, a.wait_ns)) {
-                    give_up(23);
+        for (int m = cl; m < a.tiles && n > 0 && !aborted(); m += ncl, ++seg) {
+            const uint32_t d = tmem + (uint32_t)((seg & 1) * 2 * NT);
+            if (seg >= 2 && !warp_wait(accempty + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1) ^ 1u, a.wait_ns)) {
+                give_up(23);
+                break;
+            }
+            tc_fence_after();
+            for (int kb = 0; kb < n; ++kb) {
+                if (!warp_wait(full + 8 * s, ph, a.wait_ns)) {
+                    give_up(24);
                     break;
                 }
                 tc_fence_after();
-                for (int kb = 0; kb < n; ++kb) {
-                    if (!warp_wait(full + 8 * s, ph, a.wait_ns)) {
-                        give_up(24);
-                        break;
-                    }
-                    tc_fence_after();
-                    const uint32_t sa = smem_u32(smem + s * S::STAGE), sb = sa + 2 * SM_BOX;
-                    if (elect_one()) {
+                const uint32_t sa = smem_u32(smem + s * S::STAGE), sb = sa + 2 * SM_BOX;
+                if (elect_one()) {
 #pragma unroll
-                        for (int kk = 0; kk < 4; ++kk) {
-                            const uint32_t on = kb == 0 && kk == 0 ? 0u : 1u;
-                            mma_bf16(d, sw128_desc(sa + kk * 32), sw128_desc(sb + kk * 32), idesc, on);
-                            if (f) mma_bf16(d + NT, sw128_desc(sa + kk * 32), sw128_desc(sb + S::B + kk * 32), idesc, on);
-                        }
-                        mma_commit(empty + 8 * s);
-                        if (kb + 1 == n) mma_commit(accfull + 8 * (seg & 1));
+                    for (int kk = 0; kk < 4; ++kk) {
+                        const uint32_t on = kb == 0 && kk == 0 ? 0u : 1u;
+                        mma_bf16(d, sw128_desc(sa + kk * 32), sw128_desc(sb + kk * 32), idesc, on);
+                        if (!GATE) mma_bf16(d + NT, sw128_desc(sa + kk * 32), sw128_desc(sb + S::B + kk * 32), idesc, on);
                     }
-                    __syncwarp();
-                    if (++s == STAGES) { s = 0; ph ^= 1u; }
+                    mma_commit(empty + 8 * s);
+                    if (kb + 1 == n) mma_commit(accfull + 8 * (seg & 1));
                 }
+                __syncwarp();
+                if (++s == STAGES) { s = 0; ph ^= 1u; }
             }
         }
         // all MMAs are done before the ring and TMEM are given back
@@ -277,6 +241,7 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
         const int side = quarter >> 1, r64 = (quarter & 1) * 32 + lane;
         const uint32_t to = map_rank(smem_u32(recv_mem), (uint32_t)(r64 >> 4)) + (uint32_t)(rank * S::PART + side * RT * 16 + (r64 & 15)) * 4;
         const uint32_t to_bar = map_rank(recv, (uint32_t)(r64 >> 4));
+        const bool part = kb0 < kb1;   // (none: zeros are sent, so that every CTA waits for every other one's pace)
         int seg = 0, round = 0;
         bool ok = true;
         // all four warps go on or none
@@ -286,73 +251,64 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
                          : "=r"(all) : "r"(mine && *(volatile int*)&s_abort == 0 ? 1 : 0) : "memory");
             return all != 0;
         };
-        for (int f = 0; f < 2 && ok; ++f) {
-            const SmPhase& q = a.ph[f];
-            const bool part = first_of(q, rank) < first_of(q, rank + 1);   // this CTA has a part of every tile
-            int parts = 0;
-            for (int r = 0; r < SM_S; ++r) parts += first_of(q, r) < first_of(q, r + 1) ? 1 : 0;
-            for (int m = cl; m < q.tiles && ok; m += ncl) {
-                const uint32_t d = tmem + (uint32_t)((seg & 1) * 2 * NT + (f ? side * NT : 0)) + ((uint32_t)(quarter * 32) << 16);
-                const bool done = !part || warp_wait(accfull + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1), a.wait_ns);
-                if (!done) give_up(26);
-                if (!(ok = agree(done))) break;
-                tc_fence_after();
-                const int row = m * 64 + rank * 16 + (lane & 15);   // that this CTA finishes
-                for (int t0 = 0; t0 < a.T && ok; t0 += RT, ++round) {
-                    const int b = round & 1, nt = min(RT, a.T - t0);
-                    if (part) {
-                        const uint32_t dst = to + (uint32_t)(b * S::RECV), bar = to_bar + 8 * b;
+        for (int m = cl; m < a.tiles && ok; m += ncl, ++seg) {
+            const uint32_t d = tmem + (uint32_t)((seg & 1) * 2 * NT + (GATE ? 0 : side * NT)) + ((uint32_t)(quarter * 32) << 16);
+            const bool done = !part || warp_wait(accfull + 8 * (seg & 1), (uint32_t)((seg >> 1) & 1), a.wait_ns);
+            if (!done) give_up(26);
+            if (!(ok = agree(done))) break;
+            tc_fence_after();
+            const int row = m * 64 + rank * 16 + (lane & 15);   // that this CTA finishes
+            for (int t0 = 0; t0 < a.T && ok; t0 += RT, ++round) {
+                const int b = round & 1, nt = min(RT, a.T - t0);
+                const uint32_t dst = to + (uint32_t)(b * S::RECV), bar = to_bar + 8 * b;
 #pragma unroll 1
-                        for (int i = 0; i < nt; i += 16) {
-                            float v[16];
-                            tmem_ld16(d + t0 + i, v);
+                for (int i = 0; i < nt; i += 16) {
+                    float v[16];
+                    if (part) {
+                        tmem_ld16(d + t0 + i, v);
+                    } else {
 #pragma unroll
-                            for (int e = 0; e < 16; ++e)
-                                if (i + e < nt) send(dst + (uint32_t)(i + e) * 64, v[e], bar);
-                        }
-                        if (t0 + RT >= a.T) {   // the accumulator is read
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(accempty + 8 * (seg & 1));
-                        }
+                        for (int e = 0; e < 16; ++e) v[e] = 0.f;
                     }
-                    if (threadIdx.x == 64) mbar_expect_tx(recv + 8 * b, (uint32_t)(parts * nt * 2 * 16 * 4));
-                    const bool got = warp_wait(recv + 8 * b, (uint32_t)((round >> 1) & 1), a.wait_ns);
-                    if (!got) give_up(27);
-                    const float* in = reinterpret_cast<const float*>(recv_mem + b * S::RECV);
-                    for (int i = 2 * quarter + (lane >> 4); i < nt && got; i += 8) {
-                        float v = 0.f, u = 0.f;
 #pragma unroll
-                        for (int r = 0; r < SM_S; ++r) {
-                            if (first_of(q, r) == first_of(q, r + 1)) continue;
-                            const float* at = in + r * S::PART + i * 16 + (lane & 15);
-                            v += at[0];
-                            u += at[RT * 16];
-                        }
-                        const int t = t0 + i;
-                        if (f == 0 && row < a.F) {
-                            float p, w, h;
-                            mlp_factors<ACT, 1>(&v, &u, &p, &w, &h);
-                            a.h[(int64_t)t * a.F + row] = f2bf(h);
-                            if (a.pq) {
-                                pq_put(a.pq, t, row, a.F, p);
-                                pq_put(a.pq + a.q_off, t, row, a.F, w);
-                            }
-                        } else if (f == 1 && row < a.C) {
-                            a.y[(int64_t)t * a.C + row] = f2bf(v + u);
-                        }
-                    }
-                    // The buffer is read before any of these warps sends on.  With two buffers nothing more is
-                    // needed: whoever sends round n + 2 has received n + 1, which every CTA sent after it read n.
-                    ok = agree(got);
+                    for (int e = 0; e < 16; ++e)
+                        if (i + e < nt) send(dst + (uint32_t)(i + e) * 64, v[e], bar);
                 }
-                if (part) ++seg;
-            }
-            if (f == 0) {
-                // this CTA's part of h is written (given up: counted all the same, the others need not wait long)
-                asm volatile("fence.proxy.async;" ::: "memory");   // it will be read by TMA
-                asm volatile("bar.sync 1, 128;" ::: "memory");
-                if (threadIdx.x == 64) add_release(a.cnt + SM_ARRIVE);
+                if (t0 + RT >= a.T) {   // the accumulator is read
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(accempty + 8 * (seg & 1));
+                }
+                if (threadIdx.x == 64) mbar_expect_tx(recv + 8 * b, (uint32_t)(SM_S * nt * 2 * 16 * 4));
+                __syncwarp();
+                const bool got = warp_wait(recv + 8 * b, (uint32_t)((round >> 1) & 1), a.wait_ns);
+                if (!got) give_up(27);
+                const float* in = reinterpret_cast<const float*>(recv_mem + b * S::RECV);
+                for (int i = 2 * quarter + (lane >> 4); i < nt && got; i += 8) {
+                    float v = 0.f, u = 0.f;
+#pragma unroll
+                    for (int r = 0; r < SM_S; ++r) {
+                        const float* at = in + r * S::PART + i * 16 + (lane & 15);
+                        v += at[0];
+                        u += at[RT * 16];
+                    }
+                    const int t = t0 + i;
+                    if (row >= a.out) continue;
+                    if (GATE) {
+                        float p, w, h;
+                        mlp_factors<ACT, 1>(&v, &u, &p, &w, &h);
+                        a.y[(int64_t)t * a.out + row] = f2bf(h);
+                        if (a.pq) {
+                            pq_put(a.pq, t, row, a.out, p);
+                            pq_put(a.pq + a.q_off, t, row, a.out, w);
+                        }
+                    } else {
+                        a.y[(int64_t)t * a.out + row] = f2bf(v + u);
+                    }
+                }
+                // The buffer is read before any of these warps sends on.  With two buffers nothing more is
+                // needed: whoever sends round n + 2 has received n + 1, which every CTA sent after it read n.
+                ok = agree(got);
             }
         }
     }
@@ -363,30 +319,27 @@ __global__ void __launch_bounds__(SM_NT, 1) k_mlp_small(const __grid_constant__ 
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::COLS) : "memory");
     }
-    // the last CTA to leave clears the counters for the next launch
-    if (threadIdx.x == 0 && atomicAdd(a.cnt + SM_LEAVE, 1) == (int)gridDim.x - 1) {
-        a.cnt[SM_ARRIVE] = 0;
-        a.cnt[SM_LEAVE] = 0;
-    }
 }
 
-template <int NT, int ACT>
-cudaError_t sm_launch(const SmMaps& maps, const SmArgs& a, cudaStream_t st) {
+// `follow`: placed while the launch before runs out (the second product after the first)
+template <int NT, int ACT, bool GATE>
+cudaError_t sm_launch(const SmMaps& maps, const SmArgs& a, bool follow, cudaStream_t st) {
     static std::atomic<int> fit[64];   // clusters that a device holds at once, asked for once
-    auto* k = k_mlp_small<NT, ACT>;
-    cudaError_t e = smem_optin((const void*)k, SmShape<NT>::SMEM);
+    using S = SmShape<NT, GATE>;
+    auto* k = k_mlp_small<NT, ACT, GATE>;
+    cudaError_t e = smem_optin((const void*)k, S::SMEM);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(device_sms() / SM_S * SM_S);
     cfg.blockDim = dim3(SM_NT);
-    cfg.dynamicSmemBytes = SmShape<NT>::SMEM;
+    cfg.dynamicSmemBytes = S::SMEM;
     cfg.stream = st;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = SM_S;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeCooperative;   // the CTAs wait for one another
-    at[1].val.cooperative = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
     int dev = 0, n = 0;
@@ -397,19 +350,31 @@ cudaError_t sm_launch(const SmMaps& maps, const SmArgs& a, cudaStream_t st) {
         if (n < 1) return cudaErrorInvalidConfiguration;
         if (keep) fit[dev].store(n, std::memory_order_relaxed);
     }
-    const int tiles = a.ph[0].tiles > a.ph[1].tiles ? a.ph[0].tiles : a.ph[1].tiles;
-    cfg.gridDim = dim3(SM_S * (n < tiles ? n : tiles));
-    cfg.numAttrs = 2;
+    cfg.gridDim = dim3(SM_S * (n < a.tiles ? n : a.tiles));
+    cfg.numAttrs = follow ? 2 : 1;
     e = cudaLaunchKernelEx(&cfg, k, maps, a);
     note_launch();
     return e == cudaSuccess ? cudaGetLastError() : e;
 }
 template <int NT>
-cudaError_t sm_launch_act(int act, const SmMaps& maps, const SmArgs& a, cudaStream_t st) {
-    if (act == XHC_ACT_SILU) return sm_launch<NT, XHC_ACT_SILU>(maps, a, st);
-    if (act == XHC_ACT_GELU) return sm_launch<NT, XHC_ACT_GELU>(maps, a, st);
-    return sm_launch<NT, XHC_ACT_RELU>(maps, a, st);
+cudaError_t sm_gate(int act, const SmMaps& maps, const SmArgs& a, cudaStream_t st) {
+    if (act == XHC_ACT_SILU) return sm_launch<NT, XHC_ACT_SILU, true>(maps, a, pdl_on(), st);
+    if (act == XHC_ACT_GELU) return sm_launch<NT, XHC_ACT_GELU, true>(maps, a, pdl_on(), st);
+    return sm_launch<NT, XHC_ACT_RELU, true>(maps, a, pdl_on(), st);
 }
+
+SmArgs sm_args(int T, int out, int kb, uint16_t* y, int* err) {
+    SmArgs a = {};
+    a.T = T;
+    a.out = out;
+    a.kb = kb;
+    a.tiles = (out + 63) / 64;
+    a.y = y;
+    a.wait_ns = debug_wait_ns();
+    a.err = err;
+    return a;
+}
+int sm_n(int T) { return T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128; }
 
 }  // namespace
 
@@ -418,34 +383,35 @@ cudaError_t sm_launch_act(int act, const SmMaps& maps, const SmArgs& a, cudaStre
 // at 128; C = 1024, F = 2816: 13 / 27 at 1, 20 / 21 at 64, 22 / 21 at 65; C = 264, F = 712: 8.5 / 12.3 at 1, 13 / 13 at 64.
 bool mlp_small(int64_t T, int C, int F) { return T <= ((int64_t)C * F >= (int64_t)1 << 23 ? 128 : 64); }
 
-cudaError_t launch_mlp_small(int T, int C, int F, int act, const uint16_t* x, const uint16_t* Wg, const uint16_t* Wu,
-                             const uint16_t* Wd, uint16_t* h, void* pq, uint16_t* y, int* cnt, int* err, cudaStream_t st) {
-    SmArgs a = {};
-    a.T = T;
-    a.C = C;
-    a.F = F;
-    a.ph[0] = {(C + 63) / 64, (F + 63) / 64};
-    a.ph[1] = {(F + 127) / 128, (C + 63) / 64};
-    a.cnt = cnt;
-    a.h = h;
-    a.y = y;
+cudaError_t launch_mlp_small_gate(int T, int C, int F, int act, const uint16_t* x, const uint16_t* Wg, const uint16_t* Wu,
+                                  uint16_t* h, void* pq, int* err, cudaStream_t st) {
+    SmArgs a = sm_args(T, F, (C + 63) / 64, h, err);
     a.pq = (unsigned char*)pq;
     a.q_off = (int64_t)mlp_pq_bytes(T, F);
-    a.wait_ns = debug_wait_ns();
-    a.err = err;
-    const int NT = T <= 16 ? 16 : T <= 32 ? 32 : T <= 64 ? 64 : 128;
+    const int NT = sm_n(T);
     SmMaps m;
-    if (!make_map_box(&m.gate, Wg, C, F, 64, 64) || !make_map_box(&m.up, Wu, C, F, 64, 64) ||
-        !make_map_box(&m.x, x, C, T, 64, NT))
+    if (!make_map_box(&m.w, Wg, C, F, 64, 64) || !make_map_box(&m.up, Wu, C, F, 64, 64) || !make_map_box(&m.tok, x, C, T, 64, NT))
         return cudaErrorInvalidValue;
-    a.down_blocks = F % 64 == 0;
-    if (a.down_blocks ? !map_blocks(&m.down, Wd, C, F, 64, 2) || !map_blocks(&m.h, h, T, F, NT, 2)
-                      : !make_map_box(&m.down, Wd, F, C, 64, 64) || !make_map_box(&m.h, h, F, T, 64, NT))
+    if (NT == 16) return sm_gate<16>(act, m, a, st);
+    if (NT == 32) return sm_gate<32>(act, m, a, st);
+    if (NT == 64) return sm_gate<64>(act, m, a, st);
+    return sm_gate<128>(act, m, a, st);
+}
+
+cudaError_t launch_mlp_small_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, int* err,
+                                  cudaStream_t st) {
+    SmArgs a = sm_args(T, C, (F + 127) / 128, y, err);
+    a.blocks = F % 64 == 0;
+    const int NT = sm_n(T);
+    SmMaps m;
+    if (a.blocks ? !map_blocks(&m.w, Wd, C, F, 64, 2) || !map_blocks(&m.tok, h, T, F, NT, 2)
+                 : !make_map_box(&m.w, Wd, F, C, 64, 64) || !make_map_box(&m.tok, h, F, T, 64, NT))
         return cudaErrorInvalidValue;
-    if (NT == 16) return sm_launch_act<16>(act, m, a, st);
-    if (NT == 32) return sm_launch_act<32>(act, m, a, st);
-    if (NT == 64) return sm_launch_act<64>(act, m, a, st);
-    return sm_launch_act<128>(act, m, a, st);
+    m.up = m.w;
+    if (NT == 16) return sm_launch<16, 0, false>(m, a, true, st);
+    if (NT == 32) return sm_launch<32, 0, false>(m, a, true, st);
+    if (NT == 64) return sm_launch<64, 0, false>(m, a, true, st);
+    return sm_launch<128, 0, false>(m, a, true, st);
 }
 
 }  // namespace xhc

@@ -742,11 +742,12 @@ cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, con
                             uint16_t* h, void* pq, int* err, cudaStream_t st);
 cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, int* err,
                             cudaStream_t st);
-// both products of the forward for few tokens; cnt: MLP_COUNTERS ints, zero between launches
-constexpr int MLP_COUNTERS = 2;
+// the forward's two products for few tokens; the second is launched right after the first
 bool mlp_small(int64_t T, int C, int F);   // whether these are few
-cudaError_t launch_mlp_small(int T, int C, int F, int act, const uint16_t* x, const uint16_t* Wg, const uint16_t* Wu,
-                             const uint16_t* Wd, uint16_t* h, void* pq, uint16_t* y, int* cnt, int* err, cudaStream_t st);
+cudaError_t launch_mlp_small_gate(int T, int C, int F, int act, const uint16_t* x, const uint16_t* Wg, const uint16_t* Wu,
+                                  uint16_t* h, void* pq, int* err, cudaStream_t st);
+cudaError_t launch_mlp_small_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, int* err,
+                                  cudaStream_t st);
 // dg = dh p and du = dh q of dh = dy W_down, and dW_down = dy^T h (f32: fp32, accumulate: added)
 cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uint16_t* Wd, const uint16_t* h, const void* pq,
                               uint16_t* dg, uint16_t* du, void* dWd, int f32, int accumulate, int* err, cudaStream_t st);

@@ -17,7 +17,6 @@ from . import build as _build
 
 MAX_GROUP = 4
 MAX_CONV = 3
-MLP_HEADER = 256   # XHC_MLP_HEADER_BYTES
 
 MHC, FULL, FLASH = 0, 1, 2
 STATUS = {0: "ok", 1: "invalid argument", 2: "unsupported", 3: "alignment", 4: "cuda error", 5: "timeout"}
@@ -616,9 +615,9 @@ class Mlp:
         return torch.empty(self.saved_bytes(T), dtype=torch.uint8, device=device)
 
     def alloc_workspace(self, T: int, device="cuda"):
-        """A `workspace` buffer (scratch of one call at a time), its header zeroed."""
+        """A `workspace` buffer (scratch of one call at a time), error word zeroed."""
         ws = torch.empty(self.workspace_bytes(T), dtype=torch.uint8, device=device)
-        ws[:MLP_HEADER].zero_()
+        ws[:256].zero_()
         return ws
 
     def shapes(self) -> dict:

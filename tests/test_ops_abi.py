@@ -24,7 +24,7 @@ def test_mlp_sizes_and_refusals(L):
     size = lambda C, F, act, T: L.xhc_mlp_saved_bytes(X._MlpConfig(C, F, act), T, n)
     assert size(64, 128, 0, 40) == OK
     assert n.value >= 40 * 128 * 2 + 2 * 64 * 128 * 3   # h, and p and q of whole blocks of 32 tokens
-    assert L.xhc_mlp_workspace_bytes(X._MlpConfig(64, 128, 0), 40, n) == OK and n.value >= X.MLP_HEADER + 2 * 40 * 128 * 2
+    assert L.xhc_mlp_workspace_bytes(X._MlpConfig(64, 128, 0), 40, n) == OK and n.value >= 256 + 2 * 40 * 128 * 2
     for bad in ((0, 128, 0, 1), (64, 0, 0, 1), (64, 128, 3, 1), (64, 128, -1, 1), (64, 128, 0, 0), (64, 128, 0, -5)):
         assert size(*bad) == INVALID, bad
     for bad in ((60, 128, 0, 1), (64, 132, 0, 1), (16392, 128, 0, 1), (64, 65544, 0, 1), (64, 128, 0, (1 << 24) + 1)):
