@@ -643,26 +643,27 @@ cudaError_t gm_plan(GemmArgs& a, GmPlan* pl) {
 }
 
 template <class S>
-cudaError_t gm_launch(const GemmMaps& maps, GemmArgs& a, int clusters, cudaStream_t st) {
+cudaError_t gm_launch(const GemmMaps& maps, GemmArgs& a, int clusters, bool follow, cudaStream_t st) {
     gm_tiles<S>(a, clusters);
     cudaLaunchAttribute at[2];
     cudaLaunchConfig_t cfg = gm_config<S>(at, a.tiles < clusters ? a.tiles : clusters);
     cfg.stream = st;
-    cfg.numAttrs = pdl_on() ? 2 : 1;
+    cfg.numAttrs = follow || pdl_on() ? 2 : 1;
     const cudaError_t e = cudaLaunchKernelEx(&cfg, k_mlp_gemm<S>, maps, a);
     note_launch();
     return e == cudaSuccess ? cudaGetLastError() : e;
 }
-// na, nb, no: maps that are set
-cudaError_t gm_run(GemmMaps& maps, GemmArgs& a, const GmPlan& pl, int na, int nb, int no, cudaStream_t st) {
+// na, nb, no: maps that are set; follow: the call's second launch, whose CTAs are set up while the first one's run out, in
+// a captured graph too (unlike the connection op's kernels these set up barriers, TMEM and a cluster: 0.7 us)
+cudaError_t gm_run(GemmMaps& maps, GemmArgs& a, const GmPlan& pl, int na, int nb, int no, bool follow, cudaStream_t st) {
     for (int q = na; q < 4; ++q) maps.a[q] = maps.a[0];
     for (int q = nb; q < 4; ++q) maps.b[q] = maps.b[0];
     for (int q = no; q < 3; ++q) maps.o[q] = maps.o[0];
     switch (pl.shape) {
-        case 0: return gm_launch<GmTall>(maps, a, pl.clusters, st);
-        case 1: return gm_launch<GmPair>(maps, a, pl.clusters, st);
+        case 0: return gm_launch<GmTall>(maps, a, pl.clusters, follow, st);
+        case 1: return gm_launch<GmPair>(maps, a, pl.clusters, follow, st);
     }
-    return gm_launch<GmWide>(maps, a, pl.clusters, st);
+    return gm_launch<GmWide>(maps, a, pl.clusters, follow, st);
 }
 
 GemmProb gm_prob(int M, int N, int K, int kind, int set, int out) {
@@ -726,7 +727,7 @@ cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, con
     if (!map_k(&m.a[0], x, T, C, pl.a_rows()) || !map_k(&m.b[0], Wg, F, C, pl.b_rows()) || !map_k(&m.b[1], Wu, F, C, pl.b_rows()) ||
         !map_out(&m.o[0], h, T, F, false, pl.shape < 2 ? 128 : 64))
         return cudaErrorInvalidValue;
-    return gm_run(m, a, pl, 1, 2, 1, st);
+    return gm_run(m, a, pl, 1, 2, 1, false, st);
 }
 
 cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, int* err,
@@ -739,7 +740,7 @@ cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16
     GemmMaps m = {};
     if (!map_k(&m.a[0], h, T, F, pl.a_rows()) || !map_k(&m.b[0], Wd, C, F, pl.b_rows()) || !map_out(&m.o[0], y, T, C, false, 128))
         return cudaErrorInvalidValue;
-    return gm_run(m, a, pl, 1, 1, 1, st);
+    return gm_run(m, a, pl, 1, 1, 1, true, st);
 }
 
 cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uint16_t* Wd, const uint16_t* h, const void* pq,
@@ -761,7 +762,7 @@ cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uin
         !map_out(&m.o[0], dg, T, F, false, 64) || !map_out(&m.o[1], du, T, F, false, 64) ||
         !map_out(&m.o[2], dWd, C, F, f32 != 0, 128))
         return cudaErrorInvalidValue;
-    return gm_run(m, a, pl, 2, 2, 3, st);
+    return gm_run(m, a, pl, 2, 2, 3, false, st);
 }
 
 cudaError_t launch_mlp_dx_dw(int T, int C, int F, const uint16_t* x, const uint16_t* dg, const uint16_t* du,
@@ -786,7 +787,7 @@ cudaError_t launch_mlp_dx_dw(int T, int C, int F, const uint16_t* x, const uint1
         return cudaErrorInvalidValue;
     m.b[3] = m.b[2];
     a.p[2].bmn = a.p[1].bmn;
-    return gm_run(m, a, pl, 4, 4, 3, st);
+    return gm_run(m, a, pl, 4, 4, 3, true, st);
 }
 
 }  // namespace xhc
