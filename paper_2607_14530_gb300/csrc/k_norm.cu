@@ -6,7 +6,8 @@
 // the store.  A group of up to 512 threads holds a token, 8 channels (16 bytes of bf16) a thread and chunk.  Where a token
 // is one or two rows (N = 1, and every backward) its loads are too few to fill the memory's latency, so each
 // thread copies its chunks of the next tokens into shared memory ahead (cp.async: no registers, and no other thread
-// reads them): T = 32768, N = 1, C = 4096 took 116 us forward and 147 backward with the next token in registers.  The backward
+// reads them): T = 32768, N = 1, C = 4096 takes 95 us forward (5.7 TB/s) and 141 backward (5.7); with the next token in
+// registers it took 116 and 147.  T = 2048, N = 16, C = 4096 with s kept: 52 us forward (6.1 TB/s), 55 backward.  The backward
 // reads s in fp32 as the forward left it (N = 1: X itself, which is s): 4 bytes a channel where the state has
 // 2 N.  In bf16 it would put 2^-9 into every term of dw, which is fp32.
 #include "xhc_internal.cuh"
@@ -332,8 +333,8 @@ int norm_bwd_blocks(int64_t T, int C) {
         else { LAUNCH(4); }                                  \
     } while (0)
 
-// Few tokens: all of a token's streams in flight at once (24 tokens of 16 x 4096: 3.2 us; 5.5 with 8 streams of two
-// chunks a thread).
+// Few tokens: all of a token's streams in flight at once (24 tokens of 16 x 4096: 4.0 us captured; 8 streams at a
+// time and two chunks a thread took 2.3 us more).
 cudaError_t launch_norm_fwd(int T, int N, int C, float eps, const uint16_t* X, const float* w, uint16_t* y,
                             float* sum, float* rstd, cudaStream_t st) {
     const int nt = norm_threads(C);
