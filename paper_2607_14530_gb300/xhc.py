@@ -567,6 +567,15 @@ def _arg(t, name, dtype, shape=None):
     return t.data_ptr()
 
 
+def _alloc(stream, *args, **kw):
+    """torch.empty of a call on ``stream`` (None: the current one): memory of that stream, which the caching
+    allocator hands on no earlier than in its order."""
+    if stream is None:
+        return torch.empty(*args, **kw)
+    with torch.cuda.stream(stream):
+        return torch.empty(*args, **kw)
+
+
 def _buffer(t, name, nbytes):
     """The pointer of a `saved` or `workspace` buffer (uint8, at least nbytes)."""
     p = _arg(t, name, torch.uint8)
@@ -633,7 +642,7 @@ class Mlp:
         bf, T = torch.bfloat16, x.shape[0]
         px = _arg(x, "x", bf, (T, self.C))
         if y is None:
-            y = torch.empty_like(x)
+            y = _alloc(stream, T, self.C, dtype=bf, device=x.device)
         nsaved, nws = self._bytes(T)
         W = self._weights(P, "", bf)
         _check(lib().xhc_mlp_fwd(self._c, T, W, px, _arg(y, "y", bf, (T, self.C)),
@@ -646,7 +655,7 @@ class Mlp:
         bf, T = torch.bfloat16, x.shape[0]
         px = _arg(x, "x", bf, (T, self.C))
         if dx is None:
-            dx = torch.empty_like(x)
+            dx = _alloc(stream, T, self.C, dtype=bf, device=x.device)
         nsaved, nws = self._bytes(T)
         W = self._weights(P, "", bf)
         gt = getattr(grads.get("W_gate"), "dtype", None)
@@ -704,7 +713,7 @@ class SumNorm:
         bf, T = torch.bfloat16, X.shape[0]
         pX = self._state(X, "X", T)
         if y is None:
-            y = torch.empty(T, self.C, dtype=bf, device=X.device)
+            y = _alloc(stream, T, self.C, dtype=bf, device=X.device)
         _check(lib().xhc_sum_norm_fwd(self.N, self.C, self.eps, T, pX, _arg(w, "w", torch.float32, (self.C,)),
                                       _arg(y, "y", bf, (T, self.C)),
                                       None if saved is None else _buffer(saved, "saved", self._bytes(T)[0]), _stream(stream)),
@@ -719,7 +728,7 @@ class SumNorm:
             raise XhcError("X is needed with N = 1")
         pX = None if X is None else self._state(X, "X", T)
         if dX is None:
-            dX = torch.empty((T, self.N, self.C) if X is None else X.shape, dtype=torch.bfloat16, device=dy.device)
+            dX = _alloc(stream, (T, self.N, self.C) if X is None else X.shape, dtype=torch.bfloat16, device=dy.device)
         nsaved, nws = self._bytes(T)
         _check(lib().xhc_sum_norm_bwd(self.N, self.C, T, pX, _arg(w, "w", torch.float32, (self.C,)),
                                       _arg(dy, "dy", torch.bfloat16, (T, self.C)), self._state(dX, "dX", T),
@@ -733,14 +742,18 @@ _CLIP_TYPES = frozenset((torch.float32, torch.bfloat16))
 _clip_bytes = None
 
 
-def clip_workspace(device="cuda"):
-    """A `workspace` buffer of clip_grads (scratch of one call at a time)."""
+def _clip_workspace_bytes() -> int:
     global _clip_bytes
     if _clip_bytes is None:
         n = ctypes.c_size_t()
         _check(lib().xhc_clip_workspace_bytes(ctypes.byref(n)), "xhc_clip_workspace_bytes")
         _clip_bytes = n.value
-    return torch.empty(_clip_bytes, dtype=torch.uint8, device=device)
+    return _clip_bytes
+
+
+def clip_workspace(device="cuda"):
+    """A `workspace` buffer of clip_grads (scratch of one call at a time)."""
+    return torch.empty(_clip_workspace_bytes(), dtype=torch.uint8, device=device)
 
 
 def clip_grads(grads, max_norm: float, scale: float = 1.0, eps: float = 1e-6, out=None, norm=None, ws=None, stream=None):
@@ -787,14 +800,12 @@ def clip_grads(grads, max_norm: float, scale: float = 1.0, eps: float = 1e-6, ou
         if len(set(seen)) != len(seen):
             raise XhcError("the same tensor is there twice")
     if norm is None:
-        norm = torch.empty(1, dtype=torch.float32, device="cuda")
+        norm = _alloc(stream, 1, dtype=torch.float32, device="cuda")
     if ws is None:
-        ws = clip_workspace()
-    elif _clip_bytes is None:
-        clip_workspace("cpu")
+        ws = _alloc(stream, _clip_workspace_bytes(), dtype=torch.uint8, device="cuda")
     a, c, d = array("q", ptrs), array("q", numel), array("i", [1 if t is torch.bfloat16 else 0 for t in types])
     b = None if out is None else array("q", to)
     _check(lib().xhc_clip_grads(n, a.buffer_info()[0], None if b is None else b.buffer_info()[0], c.buffer_info()[0],
                                 d.buffer_info()[0], scale, max_norm, eps, _arg(norm, "norm", torch.float32, (1,)),
-                                _buffer(ws, "ws", _clip_bytes), _stream(stream)), "xhc_clip_grads")
+                                _buffer(ws, "ws", _clip_workspace_bytes()), _stream(stream)), "xhc_clip_grads")
     return norm

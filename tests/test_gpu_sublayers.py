@@ -12,7 +12,7 @@ from torch import nn
 import op_refs as R
 from paper_2607_14530_gb300 import synth
 from paper_2607_14530_gb300.model import GatedMLP, RMSNorm, XhcStack, clip_grads_
-from paper_2607_14530_gb300.xhc import Config, Group, Mlp, SumNorm
+from paper_2607_14530_gb300.xhc import Config, Group, Mlp, SumNorm, clip_grads, clip_workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -223,3 +223,35 @@ def test_gradients_of_the_modules():
     R.assert_mlp(dict({k: getattr(m, k).grad for k in P}, y=y.detach(), dx=u.grad), ref)
     ref = R.sum_norm(x.detach(), n.w.detach(), n.op.eps, u.grad)
     R.assert_within({"y": u.detach(), "dX": x.grad, "dw": n.w.grad}, ref)
+
+
+def test_what_a_call_allocates_belongs_to_its_stream():
+    """Outputs and scratch made by a call on another stream than the current one: nothing that the current stream
+    still does with memory it has given back, or does with memory it gets next, meets them."""
+    side, m, n = torch.cuda.Stream(), Mlp(256, 520), SumNorm(4, 256)
+    P = {k: synth.normal_bf16(s, 3, std=0.05).cuda() for k, s in m.shapes().items()}
+    x, X, w = synth.normal_bf16((300, 256), 1).cuda(), synth.normal_bf16((300, 4, 256), 2).cuda(), torch.ones(256, device="cuda")
+    ws, saved, ws2, saved2 = m.alloc_workspace(300), m.alloc_saved(300), n.alloc_workspace(300), n.alloc_saved(300)
+    grads, dw = {k: torch.empty_like(v) for k, v in P.items()}, torch.empty_like(w)
+    calls = [(lambda st: m.forward(P, x, ws, saved=saved, stream=st), x),
+             (lambda st: m.backward(P, x, x, grads, saved, ws, stream=st), x),
+             (lambda st: n.forward(w, X, saved=saved2, stream=st), x),
+             (lambda st: n.backward(w, None, x, dw, saved2, ws2, stream=st), X)]
+    for call, like in calls:
+        want = call(None).clone()
+        before = torch.empty_like(like)
+        torch.cuda.synchronize()
+        torch.cuda._sleep(20_000_000)
+        before.fill_(7.0)
+        del before
+        got = call(side)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+    want = float(clip_grads([w], 1.0, out=[dw]))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    got = clip_grads([w], 1.0, out=[dw], stream=side)
+    after = [clip_workspace().fill_(0xFF) for _ in range(3)]
+    torch.cuda.synchronize()
+    assert float(got) == want and all(bool((t == 0xFF).all()) for t in after)
