@@ -1105,6 +1105,10 @@ xhc_status mlp_check(const xhc_mlp_config* c, int64_t T) {
     return XHC_OK;
 }
 
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+    return a && b && (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
 xhc_status norm_check(int N, int C, int64_t T) {
     if (N < 1 || C < 1 || T <= 0 || T > (int64_t)1 << 30) return XHC_ERR_INVALID_ARG;
     if (N > MAXN || C % 8 != 0 || C > 16384) return XHC_ERR_UNSUPPORTED;
@@ -1140,6 +1144,8 @@ xhc_status xhc_mlp_fwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
         !aligned16(saved) || !aligned16(workspace))
         return XHC_ERR_ALIGNMENT;
     const int C = cfg->C, F = cfg->F, T32 = (int)T;
+    const size_t tc = (size_t)T * C * 2;
+    if (overlap(x, tc, y, tc)) return XHC_ERR_INVALID_ARG;
     const MlpLayout L = mlp_layout(T, F);
     char *sv = (char*)saved, *ws = (char*)workspace;
     const cudaStream_t st = (cudaStream_t)stream;
@@ -1173,6 +1179,8 @@ xhc_status xhc_mlp_bwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
         !aligned16(workspace))
         return XHC_ERR_ALIGNMENT;
     const int C = cfg->C, F = cfg->F, T32 = (int)T;
+    const size_t tc = (size_t)T * C * 2;
+    if (overlap(x, tc, dx, tc) || overlap(dy, tc, dx, tc)) return XHC_ERR_INVALID_ARG;
     const MlpLayout L = mlp_layout(T, F);
     const char* sv = (const char*)saved;
     char* ws = (char*)workspace;
@@ -1210,6 +1218,7 @@ xhc_status xhc_sum_norm_fwd(int N, int C, float eps, int64_t T, const uint16_t* 
     if (s != XHC_OK) return s;
     if (!X || !w || !y || !(eps >= 0.f)) return XHC_ERR_INVALID_ARG;
     if (!aligned16(X) || !aligned16(w) || !aligned16(y) || !aligned16(saved)) return XHC_ERR_ALIGNMENT;
+    if (overlap(X, (size_t)T * N * C * 2, y, (size_t)T * C * 2)) return XHC_ERR_INVALID_ARG;
     const cudaStream_t st = (cudaStream_t)stream;
     PdlScope pdl;
     pdl.set((size_t)T * N * C * 2, st);
@@ -1228,9 +1237,11 @@ xhc_status xhc_sum_norm_bwd(int N, int C, int64_t T, const uint16_t* X, const fl
     if (!aligned16(X) || !aligned16(w) || !aligned16(dy) || !aligned16(dX) || !aligned16(dw) || !aligned16(saved) ||
         !aligned16(workspace))
         return XHC_ERR_ALIGNMENT;
+    const size_t state = (size_t)T * N * C * 2;
+    if (overlap(dy, (size_t)T * C * 2, dX, state) || (N == 1 && overlap(X, state, dX, state))) return XHC_ERR_INVALID_ARG;
     const cudaStream_t st = (cudaStream_t)stream;
     PdlScope pdl;
-    pdl.set((size_t)T * N * C * 2, st);
+    pdl.set(state, st);
     const char* sv = (const char*)saved;
     float* part = (float*)((char*)workspace + 256);
     XHC_K("sum_norm_bwd", st, launch_norm_bwd((int)T, N, C, X, N > 1 ? (const float*)(sv + al((size_t)T * 4)) : nullptr,

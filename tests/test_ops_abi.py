@@ -109,3 +109,19 @@ def test_finish_backward_clips_what_the_ranks_share(monkeypatch):
     assert chunk.finish_backward(grads) is grads and calls == [("sum", "ranks")] and chunk.grad_norm is None
     assert chunk.finish_backward(grads, max_norm=2.0, scale=0.5) is grads
     assert calls[1:] == [("sum", "ranks"), ("clip", 2.0, 0.5)] and chunk.grad_norm == "norm"
+
+
+def test_outputs_may_not_overlap_inputs(L):
+    """Refused before anything runs: the smallest overlaps at either end."""
+    c, W, G = X._MlpConfig(64, 128, 0), X._MlpWeights(A[0], A[1], A[2]), X._MlpWeights(A[3], A[4], A[5])
+    size, T = 64 * 2 * 8, 8
+    for d in (0, size - 16, 16 - size):
+        assert L.xhc_mlp_fwd(c, T, W, A[6], A[6] + d, None, A[8], None) == INVALID
+        for x, dy in ((A[6], A[7]), (A[7], A[6])):
+            assert L.xhc_mlp_bwd(c, T, W, x, dy, A[6] + d, G, 0, 0, A[9], A[8], None) == INVALID
+    for d in (0, 2 * size - 16, 16 - size):
+        assert L.xhc_sum_norm_fwd(2, 64, 1e-5, T, A[6], A[1], A[6] + d, None, None) == INVALID
+        assert L.xhc_sum_norm_bwd(2, 64, T, None, A[1], A[6] + d, A[6], A[5], 0, A[9], A[8], None) == INVALID
+    for d in (0, size - 16, 16 - size):
+        for x, dy in ((A[6], A[7]), (A[7], A[6])):
+            assert L.xhc_sum_norm_bwd(1, 64, T, x, A[1], dy, A[6] + d, A[5], 0, A[9], A[8], None) == INVALID
