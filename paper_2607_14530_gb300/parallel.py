@@ -127,9 +127,9 @@ class SequenceChunk:
         self.g.pre_bwd(t, P, X, d_input, dX, grads, saved, ws, stream)
 
     def finish_backward(self, grads: dict, max_norm: float | None = None, scale: float = 1.0):
-        """The gradients summed over the ranks; with ``max_norm`` times ``scale`` (e.g. one over the number of
-        micro-batches) and clipped (xhc.clip_grads)."""
+        """The gradients summed over the ranks, times ``scale`` (e.g. one over the number of micro-batches), and
+        with ``max_norm`` clipped (xhc.clip_grads)."""
         allreduce_grads(grads, self.group)
-        if max_norm is not None:
-            self.grad_norm = clip_grads(grads, max_norm, scale=scale)
+        if max_norm is not None or scale != 1.0:
+            self.grad_norm = clip_grads(grads, float("inf") if max_norm is None else max_norm, scale=scale)
         return grads

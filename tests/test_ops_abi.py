@@ -125,3 +125,12 @@ def test_outputs_may_not_overlap_inputs(L):
     for d in (0, size - 16, 16 - size):
         for x, dy in ((A[6], A[7]), (A[7], A[6])):
             assert L.xhc_sum_norm_bwd(1, 64, T, x, A[1], dy, A[6] + d, A[5], 0, A[9], A[8], None) == INVALID
+
+
+def test_finish_backward_scales_without_a_bound(monkeypatch):
+    calls = []
+    monkeypatch.setattr(parallel, "allreduce_grads", lambda g, group=None: g)
+    monkeypatch.setattr(parallel, "clip_grads", lambda g, most, scale=1.0: calls.append((most, scale)) or "norm")
+    chunk = parallel.SequenceChunk(None, 1, 1)
+    chunk.finish_backward({"a": torch.ones(2)}, scale=0.25)
+    assert calls == [(INF, 0.25)] and chunk.grad_norm == "norm"
