@@ -92,17 +92,17 @@ class _MlpFn(torch.autograd.Function):
         T = x.shape[0]
         saved = op.alloc_saved(T, device=x.device)
         y = op.forward({"W_gate": Wg, "W_up": Wu, "W_down": Wd}, x, _workspace(op, T, x.device), saved=saved)
-        ctx.save_for_backward(x, Wg, Wu, Wd)
-        ctx.op, ctx.saved = op, saved
+        ctx.save_for_backward(x, Wg, Wu, Wd, saved)   # `saved` too: given back when the backward has run
+        ctx.op = op
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        x, Wg, Wu, Wd = ctx.saved_tensors
+        x, Wg, Wu, Wd, saved = ctx.saved_tensors
         P = {"W_gate": Wg, "W_up": Wu, "W_down": Wd}
         grads = {n: torch.empty_like(v) for n, v in P.items()}
-        dx = ctx.op.backward(P, x, dy.contiguous(), grads, ctx.saved, _workspace(ctx.op, x.shape[0], x.device))
+        dx = ctx.op.backward(P, x, dy.contiguous(), grads, saved, _workspace(ctx.op, x.shape[0], x.device))
         return dx, grads["W_gate"], grads["W_up"], grads["W_down"], None
 
 
@@ -130,16 +130,16 @@ class _SumNormFn(torch.autograd.Function):
         saved = op.alloc_saved(X.shape[0], device=X.device)
         y = op.forward(w, X, saved=saved)
         # of several streams the sum is in `saved` (and the groups change the state in place); one is read again
-        ctx.save_for_backward(*((w, X) if op.N == 1 else (w,)))
-        ctx.op, ctx.saved, ctx.shape = op, saved, X.shape
+        ctx.save_for_backward(w, saved, *((X,) if op.N == 1 else ()))
+        ctx.op = op
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
-        w, X = ctx.saved_tensors if ctx.op.N == 1 else (*ctx.saved_tensors, None)
+        w, saved, X = ctx.saved_tensors if ctx.op.N == 1 else (*ctx.saved_tensors, None)
         dw = torch.empty_like(w)
-        dX = ctx.op.backward(w, X, dy.contiguous(), dw, ctx.saved, _workspace(ctx.op, dy.shape[0], dy.device))
+        dX = ctx.op.backward(w, X, dy.contiguous(), dw, saved, _workspace(ctx.op, dy.shape[0], dy.device))
         return _owned(dX), dw, None
 
 

@@ -255,3 +255,20 @@ def test_what_a_call_allocates_belongs_to_its_stream():
     after = [clip_workspace().fill_(0xFF) for _ in range(3)]
     torch.cuda.synchronize()
     assert float(got) == want and all(bool((t == 0xFF).all()) for t in after)
+
+
+@pytest.mark.parametrize("make", [lambda: GatedMLP(64, 2048), lambda: RMSNorm(2048, N=4)])
+def test_what_a_forward_keeps_is_given_back(make):
+    """... when its backward has run, though the output (a loss that is logged) lives on."""
+    m = make().cuda()
+    x = synth.normal_bf16((4096, 64) if isinstance(m, GatedMLP) else (4096, 4, 2048), 1).cuda().requires_grad_(True)
+    m(x).sum().backward()   # (workspaces and gradients are there from now on)
+    torch.cuda.synchronize()
+    start = torch.cuda.memory_allocated()
+    y = m(x)
+    kept = m.op.saved_bytes(4096)
+    assert torch.cuda.memory_allocated() - start >= kept
+    y.sum().backward()
+    assert torch.cuda.memory_allocated() - start < y.numel() * 2 + kept // 4
+    with pytest.raises(RuntimeError, match="second time"):
+        y.sum().backward()
