@@ -86,6 +86,21 @@ def _workspace(op, T: int, device):
     return ws
 
 
+def _leaves_on_one_stream(y):
+    """Refuses a captured pass whose leaves another, living graph holds since a different stream: autograd would add
+    their gradients on that stream, outside the capture, which ends the process.  A leaf's node keeps the stream that it was made on;
+    it lives as long as any graph does that holds it."""
+    if y.grad_fn is not None:
+        here, capturing = torch.cuda.current_stream(y.device).cuda_stream, torch.cuda.is_current_stream_capturing()
+        for node, _ in y.grad_fn.next_functions:
+            if node is None or "AccumulateGrad" not in node.name():
+                continue
+            if node.metadata.setdefault("xhc_stream", here) != here and capturing:
+                raise xhc.XhcError("a graph of the same parameters made on another stream is alive: drop its outputs "
+                                   "before a pass is captured")
+    return y
+
+
 class _MlpFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, Wg, Wu, Wd, op):
@@ -119,7 +134,7 @@ class GatedMLP(nn.Module):
     def forward(self, x):
         x = x.contiguous()
         if torch.is_grad_enabled():
-            return _MlpFn.apply(x, self.W_gate, self.W_up, self.W_down, self.op)
+            return _leaves_on_one_stream(_MlpFn.apply(x, self.W_gate, self.W_up, self.W_down, self.op))
         P = {"W_gate": self.W_gate, "W_up": self.W_up, "W_down": self.W_down}
         return self.op.forward(P, x, _workspace(self.op, x.shape[0], x.device))
 
@@ -155,7 +170,7 @@ class RMSNorm(nn.Module):
     def forward(self, x):
         x = x.contiguous()
         if torch.is_grad_enabled():
-            return _SumNormFn.apply(x, self.w, self.op)
+            return _leaves_on_one_stream(_SumNormFn.apply(x, self.w, self.op))
         return self.op.forward(self.w, x)
 
 

@@ -12,7 +12,7 @@ from torch import nn
 import op_refs as R
 from paper_2607_14530_gb300 import synth
 from paper_2607_14530_gb300.model import GatedMLP, RMSNorm, XhcStack, clip_grads_
-from paper_2607_14530_gb300.xhc import Config, Group, Mlp, SumNorm, clip_grads, clip_workspace
+from paper_2607_14530_gb300.xhc import Config, Group, Mlp, SumNorm, XhcError, clip_grads, clip_workspace
 
 pytestmark = pytest.mark.gpu
 
@@ -272,3 +272,37 @@ def test_what_a_forward_keeps_is_given_back(make):
     assert torch.cuda.memory_allocated() - start < y.numel() * 2 + kept // 4
     with pytest.raises(RuntimeError, match="second time"):
         y.sum().backward()
+
+
+def test_captured_backward():
+    """A captured training pass replays to the eager one's bits; one whose parameters are held by an eager graph
+    is refused before its backward (autograd would leave the capture)."""
+    m = nn.Sequential(RMSNorm(256), GatedMLP(256, 520)).cuda()
+    x, dy = synth.normal_bf16((100, 256), 1).cuda().requires_grad_(True), synth.normal_bf16((100, 256), 2).cuda()
+    leaves = [x, *m.parameters()]
+    y = m(x)
+    y.backward(dy)
+    want = [y.detach().clone()] + [p.grad.clone() for p in leaves]
+
+    def capture(backward):
+        g = torch.cuda.CUDAGraph()
+        for p in leaves:
+            p.grad = None
+        with torch.cuda.graph(g):
+            out = m(x)
+            if backward:
+                out.backward(dy)
+            out = out.detach()
+        return g, out
+
+    with pytest.raises(XhcError, match="alive"):
+        capture(False)
+    del y
+    g, out = capture(True)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for t in (out, *(p.grad for p in leaves)):
+            t.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip([out] + [p.grad for p in leaves], want))
