@@ -317,6 +317,12 @@ def _stream(stream):
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
+def _device_error(ws, clear):
+    code = ctypes.c_int()
+    lib().xhc_workspace_error(_ptr(ws), ctypes.byref(code), 1 if clear else 0)
+    return code.value
+
+
 class Group:
     """One connection-op group (G sublayers) bound to a libxhc handle."""
 
@@ -383,9 +389,7 @@ class Group:
 
     def device_error(self, ws, clear: bool = False) -> int:
         """The workspace's device error word (nonzero: a bounded wait gave up).  Synchronous."""
-        code = ctypes.c_int()
-        lib().xhc_workspace_error(_ptr(ws), ctypes.byref(code), 1 if clear else 0)
-        return code.value
+        return _device_error(ws, clear)
 
     def params(self, P: dict) -> _Params:
         return _fill(_Params(), P, self.cfg)
@@ -628,6 +632,10 @@ class Mlp:
         ws = torch.empty(self.workspace_bytes(T), dtype=torch.uint8, device=device)
         ws[:256].zero_()
         return ws
+
+    def device_error(self, ws, clear: bool = False) -> int:
+        """The workspace's device error word (nonzero: a bounded wait gave up).  Synchronous."""
+        return _device_error(ws, clear)
 
     def shapes(self) -> dict:
         return {"W_gate": (self.F, self.C), "W_up": (self.F, self.C), "W_down": (self.C, self.F)}

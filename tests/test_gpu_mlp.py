@@ -189,3 +189,15 @@ def test_refusals():
         op.backward(P, x, dy, grads, saved, ws, accumulate=True)
     with pytest.raises(XhcError, match="invalid"):
         op.forward(P, x[:0], ws)
+
+
+def test_device_error_word():
+    """Zero in a fresh workspace and after calls; what a wait that gave up would leave is read and cleared."""
+    x, P, dy = inputs(24, 64, 128)
+    op = Mlp(64, 128)
+    ws = op.alloc_workspace(24)
+    op.forward(P, x.cuda(), ws)
+    assert op.device_error(ws) == 0
+    ws[:4].view(torch.int32).fill_(13)
+    torch.cuda.synchronize()
+    assert op.device_error(ws) == 13 and op.device_error(ws, clear=True) == 13 and op.device_error(ws) == 0
