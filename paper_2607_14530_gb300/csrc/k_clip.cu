@@ -4,7 +4,7 @@
 // CLIP_G units, one per warp at a time: a warp finds its tensor in the table (a kernel argument: no copy to
 // the device, and a captured graph holds it), so that many small tensors share a launch and its blocks.  The
 // second pass walks the granules from the last to the first: what the first pass read last still lies in L2.
-// 151 M bf16 elements (302 MB): 55 us for the norm (5.5 TB/s), 97 for the scaling, in place.
+// 302 MB, nearly all bf16: 55 us for the norm (5.5 TB/s), 97 for the scaling, in place.
 #include "xhc_internal.cuh"
 
 namespace xhc {
