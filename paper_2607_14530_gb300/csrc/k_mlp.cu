@@ -81,7 +81,7 @@ struct GemmArgs {
     GemmProb p[3];
     int nprob, tiles;
     int na;                // tiles of the first problem: they are taken first
-    int head;              // rounds of other tiles taken by the CTAs with one tile fewer of these (gm_next)
+    int head;              // rounds of other tiles taken by the CTAs with one tile fewer of these (gm_tile_code)
     int act;
     uint64_t wait_ns;
     int* err;
@@ -134,53 +134,83 @@ __device__ __forceinline__ void gm_commit(uint32_t bar, uint16_t mask) {
         : "memory");
 }
 
-// 32 columns of a lane's row of TMEM; the wait is in the same statement
+// 32 columns of a lane's row of TMEM, or 32 at each of two places; the wait is in the same statement (the first 32 are written
+// before the second address is read)
 __device__ __forceinline__ void tmem_ld32(uint32_t ta, float* v) {
     uint32_t r[32];
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,"
-        "%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+        "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n"
         "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]),
+          "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]),
+          "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
         : "r"(ta));
 #pragma unroll
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
+__device__ __forceinline__ void tmem_ld32x2(uint32_t ta, float* v, uint32_t tb, float* u) {
+    uint32_t r[64];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,"
+        "%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%64];\n"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,%48,%49,%50,%51,%52,%53,"
+        "%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%65];\n"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=&r"(r[0]), "=&r"(r[1]), "=&r"(r[2]), "=&r"(r[3]), "=&r"(r[4]), "=&r"(r[5]), "=&r"(r[6]), "=&r"(r[7]),
+          "=&r"(r[8]), "=&r"(r[9]), "=&r"(r[10]), "=&r"(r[11]), "=&r"(r[12]), "=&r"(r[13]), "=&r"(r[14]), "=&r"(r[15]),
+          "=&r"(r[16]), "=&r"(r[17]), "=&r"(r[18]), "=&r"(r[19]), "=&r"(r[20]), "=&r"(r[21]), "=&r"(r[22]), "=&r"(r[23]),
+          "=&r"(r[24]), "=&r"(r[25]), "=&r"(r[26]), "=&r"(r[27]), "=&r"(r[28]), "=&r"(r[29]), "=&r"(r[30]), "=&r"(r[31]),
+          "=r"(r[32]), "=r"(r[33]), "=r"(r[34]), "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]),
+          "=r"(r[40]), "=r"(r[41]), "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]),
+          "=r"(r[48]), "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]), "=r"(r[63])
+        : "r"(ta), "r"(tb));
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        v[i] = __uint_as_float(r[i]);
+        u[i] = __uint_as_float(r[32 + i]);
+    }
+}
 
 struct GmTile {
-    int p, m, n;   // problem, tile row, tile column
+    int p, m, n;   // problem (-1: no more tiles), tile row, tile column
 };
-__device__ __forceinline__ GmTile gm_tile(const GemmArgs& a, int t) {
-    GmTile r;
-    r.p = 0;
-    while (r.p + 1 < a.nprob && t >= a.p[r.p + 1].first) ++r.p;
-    const GemmProb& q = a.p[r.p];
+// Tile i = 0, 1, ... of cluster c of nc, as p | n | m in 4, 12 and 16 bits (-1: no more).  The first problem's, whose
+// tiles take longest, go round first; in the round that does not fill the GPU the clusters left out take
+// `head` rounds of the other problems' tiles, about as long as one of these; then all go on.
+__device__ __forceinline__ int gm_tile_code(const GemmArgs& a, int c, int nc, int i) {
+    const int whole = a.na / nc, hi = a.na - whole * nc;   // clusters c < hi have one more
+    const int mine = whole + (c < hi ? 1 : 0);
+    int t;
+    if (i < mine) {
+        t = c + i * nc;
+    } else {
+        i -= mine;
+        if (c >= hi && i < a.head) {
+            t = a.na + i * (nc - hi) + (c - hi);
+        } else {
+            if (c >= hi) i -= a.head;
+            t = a.na + a.head * (nc - hi) + i * nc + c;
+        }
+        if (t >= a.tiles) return -1;
+    }
+    int p = 0;
+    while (p + 1 < a.nprob && t >= a.p[p + 1].first) ++p;
+    const GemmProb& q = a.p[p];
     t -= q.first;
     const int per = q.group * q.tn, g = t / per, rows = min(q.group, q.tm - g * q.group);
     t -= g * per;
-    r.n = t / rows;
-    r.m = g * q.group + t - r.n * rows;
-    return r;
+    const int n = t / rows;
+    return p << 28 | n << 16 | (g * q.group + t - n * rows);
 }
-// The tiles of cluster c of nc, one after the other (i = 0, 1, ...; -1: no more).  The first problem's, whose
-// tiles take longest, go round first; in the round that does not fill the GPU the clusters left out take
-// `head` rounds of the other problems' tiles, about as long as one of these; then all go on.
-__device__ __forceinline__ int gm_next(const GemmArgs& a, int c, int nc, int i) {
-    const int whole = a.na / nc, hi = a.na - whole * nc;   // clusters c < hi have one more
-    const int mine = whole + (c < hi ? 1 : 0);
-    if (i < mine) return c + i * nc;
-    i -= mine;
-    int t;
-    if (c >= hi && i < a.head) {
-        t = a.na + i * (nc - hi) + (c - hi);
-    } else {
-        if (c >= hi) i -= a.head;
-        t = a.na + a.head * (nc - hi) + i * nc + c;
-    }
-    return t < a.tiles ? t : -1;
+// The same for a whole warp that walks its tiles: lane l works out tile i + l, once in 32 tiles.  (Each tile by itself,
+// with its divisions and reads of the problem's fields, cost every role 1000 clocks a tile.)
+__device__ __forceinline__ GmTile gm_next(const GemmArgs& a, int c, int nc, int i, int lane, int& ahead) {
+    if ((i & 31) == 0) ahead = gm_tile_code(a, c, nc, i + lane);
+    const int code = __shfl_sync(0xffffffffu, ahead, i & 31);
+    return {code < 0 ? -1 : code >> 28, code & 0xffff, (code >> 16) & 0xfff};
 }
 
 // A warp's staged 32 rows go out; what lies past the output's edges is cut off.
@@ -305,8 +335,9 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
         using K = std::integral_constant<int, K_MAJOR>;
         using R = std::integral_constant<int, MN_ROWS>;
         using Z = std::integral_constant<int, MN_BLOCKS>;
-        for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
-            const GmTile tl = gm_tile(a, t);
+        for (int i = 0, ahead; !aborted(); ++i) {
+            const GmTile tl = gm_next(a, c0, nc, i, lane, ahead);
+            if (tl.p < 0) break;
             const GemmProb& q = a.p[tl.p];
             const bool gate = q.kind == GM_GATE;
             const int m0 = (tl.m * S::PM + pm) * 256 + half * 128;
@@ -348,8 +379,10 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
         if (half == 0) {
             int s = 0;
             uint32_t ph = 0;
-            for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
-                const GemmProb& q = a.p[gm_tile(a, t).p];
+            for (int i = 0, ahead; !aborted(); ++i) {
+                const GmTile tl = gm_next(a, c0, nc, i, lane, ahead);
+                if (tl.p < 0) break;
+                const GemmProb& q = a.p[tl.p];
                 const bool amn = q.amn != 0, bmn = q.bmn != 0;
                 const int kbs = q.kb, buf = i & 1;
                 const uint32_t idesc = idesc_bf16(256, BN, amn) | ((bmn ? 1u : 0u) << 16);
@@ -404,8 +437,9 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
         };
-        for (int i = 0, t; (t = gm_next(a, c0, nc, i)) >= 0 && !aborted(); ++i) {
-            const GmTile tl = gm_tile(a, t);
+        for (int i = 0, ahead; !aborted(); ++i) {
+            const GmTile tl = gm_next(a, c0, nc, i, lane, ahead);
+            if (tl.p < 0) break;
             const GemmProb& pr = a.p[tl.p];
             const int kind = pr.kind, N = pr.N, out = pr.out, buf = i & 1;
             const int tn = kind == GM_GATE ? BN / 2 : BN, w = tn / 2;          // the tile's and this warp's columns
@@ -439,11 +473,10 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
             }
             for (int c = 0; c < end; c += 32) {
                 const bool last = c + 32 >= end;
-                float v[32];
-                tmem_ld32(acc + c, v);
+                float v[32], u[32];
+                if (kind == GM_GATE) tmem_ld32x2(acc + c, v, acc + tn + c, u);
+                else tmem_ld32(acc + c, v);
                 if (kind == GM_GATE) {
-                    float u[32];
-                    tmem_ld32(acc + tn + c, u);
                     if (last) release();
                     // 64 columns of h are staged, then stored (a warp has 32 at BN = 128)
                     const int o0 = BN == 256 ? c & 32 : 0;
@@ -546,7 +579,7 @@ using GmTall = GmShape<2, 1, 256>;
 using GmPair = GmShape<1, 1, 256>;
 using GmWide = GmShape<1, 2, 128>;
 
-// Tiles of all problems, and the order of gm_next
+// Tiles of all problems, and the order of gm_tile_code
 template <class S>
 void gm_tiles(GemmArgs& a, int clusters) {
     a.tiles = 0;
@@ -620,7 +653,7 @@ cudaError_t gm_try(GemmArgs& a, int shape, int per, int tile, GmPlan* best) {
     if (n < 1) return cudaSuccess;
     gm_tiles<S>(a, n);
     const int nc = a.tiles < n ? a.tiles : n;
-    // the first problem's tiles go round, then the rest (gm_next)
+    // the first problem's tiles go round, then the rest (gm_tile_code)
     const int64_t ta = (int64_t)a.p[0].kb * per + tile, tb = a.nprob > 1 ? (int64_t)a.p[1].kb * per + tile : 0;
     const int whole = a.na / nc, hi = a.na % nc, rest = a.tiles - a.na - a.head * (nc - hi), r = rest / nc, one = rest % nc;
     const int64_t lo = whole * ta + (a.head + r + (one > hi ? 1 : 0)) * tb;

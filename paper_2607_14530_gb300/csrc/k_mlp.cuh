@@ -85,23 +85,51 @@ __device__ __forceinline__ void pq_put(unsigned char* pq, int row, int col, int 
     blk[512 + (row & 31) * 8 + (col & 7)] = (unsigned char)(u >> 8);
 }
 
-// q = act(g), p = u act'(g) and h = q u of n columns; exponentials and quotients in the fast forms (2^-21 or
-// so), far below the stored precision.  Where an exponential overflows the sigmoid is 0, as it should be.
+// 2^v, 1 / v and the larger of two (NaN if one is), one instruction each; the first two to 2^-22 or so, subnormals as zero
+__device__ __forceinline__ float fast_exp2(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float fast_rcp(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// q = act(g), p = u act'(g) and h = q u of n columns, good to 2^-19 or so, far below the stored precision: a tile's
+// epilogue has to fit under the next one's products.  Where an exponential overflows the sigmoid is 0, as it should be.
+// GELU: Phi(-z) = e^(-z^2 / 2) R(t) t with t = 1 / (1 + 0.36 z) for z >= 0, where R is smooth from t = 1 (z = 0) to 0 (infinity):
+// a polynomial fitted to the quotient, relative error 9e-7 over the whole range.  The exponential is the derivative's
+// too.
 template <int ACT, int n = 8>
 __device__ __forceinline__ void mlp_factors(const float* g, const float* u, float* p, float* q, float* h) {
 #pragma unroll
     for (int e = 0; e < n; ++e) {
         float dq;
         if (ACT == XHC_ACT_SILU) {
-            const float s = __fdividef(1.0f, 1.0f + __expf(-g[e]));
+            const float s = fast_rcp(1.0f + fast_exp2(-1.44269504f * g[e]));
             q[e] = g[e] * s;
             dq = s + q[e] * (1.0f - s);
         } else if (ACT == XHC_ACT_GELU) {
-            const float c = normcdff(g[e]);
+            const float t = fast_rcp(fmaf(0.36f, fabsf(g[e]), 1.0f));
+            const float x = fast_exp2(-0.72134752f * g[e] * g[e]);
+            float r = fmaf(t, 0.04705620929598808f, -0.17976443469524384f);
+            r = fmaf(r, t, 0.18095368146896362f);
+            r = fmaf(r, t, 0.026549549773335457f);
+            r = fmaf(r, t, 0.1397191882133484f);
+            r = fmaf(r, t, 0.14177246391773224f);
+            r = fmaf(r, t, 0.14371304214000702f);
+            const float w = r * t * x, c = g[e] > 0.f ? 1.0f - w : w;
             q[e] = g[e] * c;
-            dq = c + g[e] * 0.3989422804f * __expf(-0.5f * g[e] * g[e]);
+            dq = fmaf(g[e] * 0.3989422804f, x, c);
         } else {
-            q[e] = g[e] > 0.f ? g[e] : g[e] != g[e] ? g[e] : 0.f;
+            q[e] = max_nan(g[e], 0.f);
             dq = g[e] > 0.f ? 1.f : 0.f;
         }
         p[e] = u[e] * dq;
