@@ -49,6 +49,8 @@ struct GmShape {
     static constexpr int STAGES = BN == 256 ? 6 : 8;
     static constexpr int SMEM = STAGES * STAGE + GM_EW * GM_STORE + (2 * STAGES + 5) * 8 + 16 + 1024;
     static constexpr int GROUP = 8 / PM;   // tile rows walked together: their B tiles are shared in L2
+    // measured clocks of a stage, and of what of a tile does not run under another's products
+    static constexpr int PER = BN == 128 ? 385 : PM == 2 ? 560 : 565, TILE = BN == 128 ? 2500 : 4000;
 };
 
 // what becomes of an accumulator
@@ -80,8 +82,8 @@ struct GemmProb {
 struct GemmArgs {
     GemmProb p[3];
     int nprob, tiles;
-    int na;                // tiles of the first problem: they are taken first
-    int head;              // rounds of other tiles taken by the CTAs with one tile fewer of these (gm_tile_code)
+    int na;                // the longer tiles, of the first problems: they are taken first
+    int head;              // rounds of other tiles taken by the clusters with one tile fewer of these (gm_tile_code)
     int act;
     uint64_t wait_ns;
     int* err;
@@ -177,9 +179,9 @@ __device__ __forceinline__ void tmem_ld32x2(uint32_t ta, float* v, uint32_t tb, 
 struct GmTile {
     int p, m, n;   // problem (-1: no more tiles), tile row, tile column
 };
-// Tile i = 0, 1, ... of cluster c of nc, as p | n | m in 4, 12 and 16 bits (-1: no more).  The first problem's, whose
-// tiles take longest, go round first; in the round that does not fill the GPU the clusters left out take
-// `head` rounds of the other problems' tiles, about as long as one of these; then all go on.
+// Tile i = 0, 1, ... of cluster c of nc, as p | n | m in 4, 12 and 16 bits (-1: no more).  The longer tiles go round
+// first; in the round that does not fill the GPU the clusters left out take `head` rounds of the others; then all
+// go on, the last clusters first.
 __device__ __forceinline__ int gm_tile_code(const GemmArgs& a, int c, int nc, int i) {
     const int whole = a.na / nc, hi = a.na - whole * nc;   // clusters c < hi have one more
     const int mine = whole + (c < hi ? 1 : 0);
@@ -192,7 +194,7 @@ __device__ __forceinline__ int gm_tile_code(const GemmArgs& a, int c, int nc, in
             t = a.na + i * (nc - hi) + (c - hi);
         } else {
             if (c >= hi) i -= a.head;
-            t = a.na + a.head * (nc - hi) + i * nc + c;
+            t = a.na + a.head * (nc - hi) + i * nc + (nc - 1 - c);
         }
         if (t >= a.tiles) return -1;
     }
@@ -579,10 +581,12 @@ using GmTall = GmShape<2, 1, 256>;
 using GmPair = GmShape<1, 1, 256>;
 using GmWide = GmShape<1, 2, 128>;
 
-// Tiles of all problems, and the order of gm_tile_code
+// Tiles of all problems (those with the longer sums come first), the order of gm_tile_code, and the busiest
+// cluster's clocks.  (The input gradients' tiles first whatever their length, and as many rounds of the others as
+// fit into one of them: at T = 8192, C = 1024, F = 2816 the busiest cluster had 45 % more than an even share.)
 template <class S>
-void gm_tiles(GemmArgs& a, int clusters) {
-    a.tiles = 0;
+int64_t gm_tiles(GemmArgs& a, int clusters) {
+    a.tiles = a.na = 0;
     for (int p = 0; p < a.nprob; ++p) {
         GemmProb& q = a.p[p];
         const int bm = 256 * S::PM, tn = (q.kind == GM_GATE ? S::BN / 2 : S::BN) * S::PN;
@@ -591,16 +595,26 @@ void gm_tiles(GemmArgs& a, int clusters) {
         q.group = S::GROUP;
         q.first = a.tiles;
         a.tiles += q.tm * q.tn;
+        if (q.kb == a.p[0].kb) a.na = a.tiles;
     }
-    a.na = a.p[0].tm * a.p[0].tn;
+    const int nc = a.tiles < clusters ? a.tiles : clusters, whole = a.na / nc, hi = a.na % nc, lo = nc - hi, nb = a.tiles - a.na;
+    const int64_t ta = (int64_t)a.p[0].kb * S::PER + S::TILE, tb = (int64_t)a.p[a.nprob - 1].kb * S::PER + S::TILE;
+    int64_t best = -1;
     a.head = 0;
-    const int nc = a.tiles < clusters ? a.tiles : clusters, left = nc - a.na % nc;
-    if (a.nprob > 1 && left < nc) {
-        // k-blocks, and about 8 for a tile's own start and end
-        a.head = (a.p[0].kb + 8) / (a.p[1].kb + 8);
-        const int most = (a.tiles - a.na) / left;
-        if (a.head > most) a.head = most;
+    for (int64_t h = hi ? ta / tb : 0, end = hi ? h + 1 : h; h <= end && h * lo <= nb; ++h) {
+        const int64_t rest = nb - h * lo, r = rest / nc, one = rest % nc;
+        const int64_t l = whole * ta + (h + r + (one > 0 ? 1 : 0)) * tb;
+        const int64_t u = hi ? (whole + 1) * ta + (r + (one > lo ? 1 : 0)) * tb : 0;
+        if (best < 0 || (l > u ? l : u) < best) {
+            best = l > u ? l : u;
+            a.head = (int)h;
+        }
     }
+    if (best < 0) {   // fewer of the others than would fill it: the clusters left out take them all
+        a.head = nb / lo;
+        best = (whole + (hi ? 1 : 0)) * ta;
+    }
+    return best;
 }
 
 template <class S>
@@ -628,8 +642,7 @@ struct GmPlan {
 };
 
 // Clusters that the GPU holds at once (an SM without partners in its group of SMs takes none: the driver says how
-// many fit, 76 pairs or 36 fours of 152 SMs), and the busiest one's clocks: `per` for a stage of 64
-// k-elements and `tile` for what of a tile does not run under another's products.
+// many fit, 76 pairs or 36 fours of 152 SMs)
 template <class S>
 cudaError_t gm_fit(int* n) {
     static std::atomic<int> fit[64];   // of a device, asked for once: the answer takes microseconds
@@ -645,20 +658,13 @@ cudaError_t gm_fit(int* n) {
     return e;
 }
 template <class S>
-cudaError_t gm_try(GemmArgs& a, int shape, int per, int tile, GmPlan* best) {
+cudaError_t gm_try(GemmArgs& a, int shape, GmPlan* best) {
     cudaError_t e = smem_optin((const void*)k_mlp_gemm<S>, S::SMEM);
     if (e != cudaSuccess) return e;
     int n = 0;
     if ((e = gm_fit<S>(&n)) != cudaSuccess) return e;
     if (n < 1) return cudaSuccess;
-    gm_tiles<S>(a, n);
-    const int nc = a.tiles < n ? a.tiles : n;
-    // the first problem's tiles go round, then the rest (gm_tile_code)
-    const int64_t ta = (int64_t)a.p[0].kb * per + tile, tb = a.nprob > 1 ? (int64_t)a.p[1].kb * per + tile : 0;
-    const int whole = a.na / nc, hi = a.na % nc, rest = a.tiles - a.na - a.head * (nc - hi), r = rest / nc, one = rest % nc;
-    const int64_t lo = whole * ta + (a.head + r + (one > hi ? 1 : 0)) * tb;
-    const int64_t up = hi ? (whole + 1) * ta + (r + (one ? 1 : 0)) * tb : 0;
-    const int64_t clocks = lo > up ? lo : up;
+    const int64_t clocks = gm_tiles<S>(a, n);
     if (best->clocks < 0 || clocks < best->clocks) {
         best->shape = shape;
         best->clusters = n;
@@ -669,9 +675,9 @@ cudaError_t gm_try(GemmArgs& a, int shape, int per, int tile, GmPlan* best) {
 
 cudaError_t gm_plan(GemmArgs& a, GmPlan* pl) {
     *pl = {-1, 0, -1};
-    cudaError_t e = gm_try<GmTall>(a, 0, 560, 4000, pl);
-    if (e == cudaSuccess) e = gm_try<GmPair>(a, 1, 565, 4000, pl);
-    if (e == cudaSuccess) e = gm_try<GmWide>(a, 2, 385, 2500, pl);
+    cudaError_t e = gm_try<GmTall>(a, 0, pl);
+    if (e == cudaSuccess) e = gm_try<GmPair>(a, 1, pl);
+    if (e == cudaSuccess) e = gm_try<GmWide>(a, 2, pl);
     return e == cudaSuccess && pl->shape < 0 ? cudaErrorInvalidConfiguration : e;
 }
 
@@ -805,21 +811,23 @@ cudaError_t launch_mlp_dx_dw(int T, int C, int F, const uint16_t* x, const uint1
     const int kind = !f32 ? GM_BF16 : accumulate ? GM_ADD : GM_F32;
     GemmProb d = gm_prob(T, C, F, GM_BF16, 0, 0);
     d.kb = 2 * d.kb1;
-    a.p[0] = d;
-    a.p[1] = gm_prob(F, C, T, kind, 2, 1);
-    a.p[2] = gm_prob(F, C, T, kind, 3, 2);
+    const GemmProb w = gm_prob(F, C, T, kind, 2, 1), v = gm_prob(F, C, T, kind, 3, 2);
+    const int id = d.kb >= w.kb ? 0 : 2, ig = d.kb >= w.kb ? 1 : 0;   // the longer tiles first
+    a.p[id] = d;
+    a.p[ig] = w;
+    a.p[ig + 1] = v;
     GmPlan pl;
     const cudaError_t e = gm_plan(a, &pl);
     if (e != cudaSuccess) return e;
     GemmMaps m = {};
-    if (!map_k(&m.a[0], dg, T, F, pl.a_rows()) || !map_k(&m.a[1], du, T, F, pl.a_rows()) || !map_mn(&m.b[0], Wg, F, C, pl.b_rows(), &a.p[0].bmn) ||
-        !map_mn(&m.b[1], Wu, F, C, pl.b_rows(), &a.p[0].bmn) || !map_mn(&m.a[2], dg, T, F, pl.a_rows(), &a.p[1].amn) ||
-        !map_mn(&m.a[3], du, T, F, pl.a_rows(), &a.p[2].amn) || !map_mn(&m.b[2], x, T, C, pl.b_rows(), &a.p[1].bmn) ||
+    if (!map_k(&m.a[0], dg, T, F, pl.a_rows()) || !map_k(&m.a[1], du, T, F, pl.a_rows()) || !map_mn(&m.b[0], Wg, F, C, pl.b_rows(), &a.p[id].bmn) ||
+        !map_mn(&m.b[1], Wu, F, C, pl.b_rows(), &a.p[id].bmn) || !map_mn(&m.a[2], dg, T, F, pl.a_rows(), &a.p[ig].amn) ||
+        !map_mn(&m.a[3], du, T, F, pl.a_rows(), &a.p[ig + 1].amn) || !map_mn(&m.b[2], x, T, C, pl.b_rows(), &a.p[ig].bmn) ||
         !map_out(&m.o[0], dx, T, C, false, 128) || !map_out(&m.o[1], dWg, F, C, f32 != 0, 128) ||
         !map_out(&m.o[2], dWu, F, C, f32 != 0, 128))
         return cudaErrorInvalidValue;
     m.b[3] = m.b[2];
-    a.p[2].bmn = a.p[1].bmn;
+    a.p[ig + 1].bmn = a.p[ig].bmn;
     return gm_run(m, a, pl, 4, 4, 3, true, st);
 }
 
