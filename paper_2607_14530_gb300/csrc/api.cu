@@ -1083,10 +1083,10 @@ namespace {
 // `saved` and `workspace` of the gated feed-forward block
 struct MlpLayout {
     size_t h, pq, saved_total;                // saved: bf16 [T][F], then p and q (mlp_pq_bytes each)
-    size_t err, hs, dg, du, ws_total;         // workspace: h of a forward without `saved` where dg is
+    size_t err, hs, dg, du, part, ws_total;   // workspace: h of a forward without `saved` where dg is; mlp_part_bytes
 };
 
-MlpLayout mlp_layout(int64_t T, int F) {
+MlpLayout mlp_layout(int64_t T, int C, int F) {
     MlpLayout L;
     const size_t tf = al((size_t)T * F * 2);
     L.h = 0;
@@ -1095,7 +1095,8 @@ MlpLayout mlp_layout(int64_t T, int F) {
     L.err = 0;
     L.hs = L.dg = 256;
     L.du = L.dg + tf;
-    L.ws_total = L.du + tf;
+    L.part = L.du + tf;
+    L.ws_total = L.part + al(mlp_part_bytes(T, C));
     return L;
 }
 
@@ -1123,7 +1124,7 @@ xhc_status xhc_mlp_saved_bytes(const xhc_mlp_config* cfg, int64_t T, size_t* byt
     const xhc_status s = mlp_check(cfg, T);
     if (s != XHC_OK) return s;
     if (!bytes) return XHC_ERR_INVALID_ARG;
-    *bytes = mlp_layout(T, cfg->F).saved_total;
+    *bytes = mlp_layout(T, cfg->C, cfg->F).saved_total;
     return XHC_OK;
 }
 
@@ -1131,7 +1132,7 @@ xhc_status xhc_mlp_workspace_bytes(const xhc_mlp_config* cfg, int64_t T, size_t*
     const xhc_status s = mlp_check(cfg, T);
     if (s != XHC_OK) return s;
     if (!bytes) return XHC_ERR_INVALID_ARG;
-    *bytes = mlp_layout(T, cfg->F).ws_total;
+    *bytes = mlp_layout(T, cfg->C, cfg->F).ws_total;
     return XHC_OK;
 }
 
@@ -1146,7 +1147,7 @@ xhc_status xhc_mlp_fwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
     const int C = cfg->C, F = cfg->F, T32 = (int)T;
     const size_t tc = (size_t)T * C * 2;
     if (overlap(x, tc, y, tc)) return XHC_ERR_INVALID_ARG;
-    const MlpLayout L = mlp_layout(T, F);
+    const MlpLayout L = mlp_layout(T, C, F);
     char *sv = (char*)saved, *ws = (char*)workspace;
     const cudaStream_t st = (cudaStream_t)stream;
     PdlScope pdl;
@@ -1161,7 +1162,7 @@ xhc_status xhc_mlp_fwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
     }
     XHC_K("mlp_gate", st, launch_mlp_gate(T32, C, F, cfg->act, x, W->gate, W->up, h,
                                           sv ? sv + L.pq : nullptr, err, st));
-    XHC_K("mlp_down", st, launch_mlp_down(T32, C, F, h, W->down, y, err, st));
+    XHC_K("mlp_down", st, launch_mlp_down(T32, C, F, h, W->down, y, (float*)(ws + L.part), err, st));
     return XHC_OK;
 }
 
@@ -1181,7 +1182,7 @@ xhc_status xhc_mlp_bwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
     const int C = cfg->C, F = cfg->F, T32 = (int)T;
     const size_t tc = (size_t)T * C * 2;
     if (overlap(x, tc, dx, tc) || overlap(dy, tc, dx, tc)) return XHC_ERR_INVALID_ARG;
-    const MlpLayout L = mlp_layout(T, F);
+    const MlpLayout L = mlp_layout(T, C, F);
     const char* sv = (const char*)saved;
     char* ws = (char*)workspace;
     const cudaStream_t st = (cudaStream_t)stream;
@@ -1192,7 +1193,8 @@ xhc_status xhc_mlp_bwd(const xhc_mlp_config* cfg, int64_t T, const xhc_mlp_weigh
     const int f32 = grad_dtype == XHC_F32;
     XHC_K("mlp_dh_dwd", st, launch_mlp_dh_dwd(T32, C, F, dy, W->down, (const uint16_t*)(sv + L.h), sv + L.pq, dg, du,
                                               g->down, f32, accumulate, err, st));
-    XHC_K("mlp_dx_dw", st, launch_mlp_dx_dw(T32, C, F, x, dg, du, W->gate, W->up, dx, g->gate, g->up, f32, accumulate, err, st));
+    XHC_K("mlp_dx_dw", st, launch_mlp_dx_dw(T32, C, F, x, dg, du, W->gate, W->up, dx, g->gate, g->up, f32, accumulate,
+                                            (float*)(ws + L.part), err, st));
     return XHC_OK;
 }
 

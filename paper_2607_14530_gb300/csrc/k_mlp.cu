@@ -77,6 +77,8 @@ struct GemmProb {
     int kb1, kb;       // k-blocks of the first operand pair, and of both
     int group;         // tile rows walked together
     int set, out;      // its first operand maps and output map
+    int split, shift;  // > 1: parts of the sum, each a tile of its own, 2^shift of every operand pair (kb: the longest)
+    int part_tm, part_rows;   // tile rows and output rows of a part
     int kind, amn, bmn;   // the operands' order
 };
 struct GemmArgs {
@@ -215,6 +217,17 @@ __device__ __forceinline__ GmTile gm_next(const GemmArgs& a, int c, int nc, int 
     return {code < 0 ? -1 : code >> 28, code & 0xffff, (code >> 16) & 0xfff};
 }
 
+// What a tile sums: kb k-blocks, the first n of them from k0 on of operand pair `set`, the rest of the next pair; its tile
+// row and, in a split product, where its part's rows begin
+struct GmSpan {
+    int m, set, k0, n, kb, row;
+};
+__device__ __forceinline__ GmSpan gm_span(const GemmProb& q, int m) {
+    if (q.split <= 1) return {m, q.set, 0, q.kb1, q.kb, 0};
+    const int s = m / q.part_tm, j = s & ((1 << q.shift) - 1), k0 = q.kb1 * j >> q.shift, n = (q.kb1 * (j + 1) >> q.shift) - k0;
+    return {m - s * q.part_tm, q.set + (s >> q.shift), k0, n, n, s * q.part_rows};
+}
+
 // A warp's staged 32 rows go out; what lies past the output's edges is cut off.
 __device__ __forceinline__ void gm_store(const CUtensorMap* map, uint32_t src, int x, int y) {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"((uint64_t)map),
@@ -292,9 +305,9 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
         const uint16_t mates = (uint16_t)(0x5u << half);   // this half's CTAs of both pairs
         int s = 0, issued = 0;
         uint32_t ph = 0;
-        // k-blocks 0 .. n - 1 of one operand pair; the operands' orders at compile time: this loop's own
+        // k-blocks first .. first + n - 1 of one operand pair; the operands' orders at compile time: this loop's own
         // instructions are what a stage costs this thread
-        auto stream = [&](auto ao, auto bo, const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int n) {
+        auto stream = [&](auto ao, auto bo, const CUtensorMap* ma, const CUtensorMap* mb, int m0, int n0, int first, int n) {
             constexpr int AO = decltype(ao)::value, BO = decltype(bo)::value;
             auto load = [&](auto order, uint32_t dst, const CUtensorMap* m, int at, int k0, int blk, uint32_t bar, bool shared) {
                 constexpr int O = decltype(order)::value;
@@ -308,7 +321,7 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
                     else gm_load(dst, m, x, y, bar);
                 }
             };
-            for (int k0 = 0; k0 < n * GM_BK; k0 += GM_BK) {
+            for (int k0 = first * GM_BK; k0 < (first + n) * GM_BK; k0 += GM_BK) {
                 if (issued >= STAGES && !warp_wait(empty + 8 * s, ph ^ 1, a.wait_ns)) {
                     give_up(11);
                     return;
@@ -342,21 +355,22 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
             if (tl.p < 0) break;
             const GemmProb& q = a.p[tl.p];
             const bool gate = q.kind == GM_GATE;
-            const int m0 = (tl.m * S::PM + pm) * 256 + half * 128;
+            const GmSpan sp = gm_span(q, tl.m);
+            const int m0 = (sp.m * S::PM + pm) * 256 + half * 128;
             // gate rows in the even CTA, up rows in the odd one: the halves of the accumulator's columns
             const int n0 = gate ? (tl.n * S::PN + pn) * (BN / 2) : (tl.n * S::PN + pn) * BN + half * (BN / 2);
-            for (int set = q.set, n = q.kb1, left = q.kb; left > 0 && !aborted(); left -= n, n = left, ++set) {
+            for (int set = sp.set, n = sp.n, left = sp.kb; left > 0 && !aborted(); left -= n, n = left, ++set) {
                 const CUtensorMap *ma = &maps.a[set], *mb = &maps.b[gate ? half : set];
                 if (q.amn == K_MAJOR) {
-                    if (q.bmn == K_MAJOR) stream(K{}, K{}, ma, mb, m0, n0, n);
-                    else if (q.bmn == MN_ROWS) stream(K{}, R{}, ma, mb, m0, n0, n);
-                    else stream(K{}, Z{}, ma, mb, m0, n0, n);
+                    if (q.bmn == K_MAJOR) stream(K{}, K{}, ma, mb, m0, n0, sp.k0, n);
+                    else if (q.bmn == MN_ROWS) stream(K{}, R{}, ma, mb, m0, n0, sp.k0, n);
+                    else stream(K{}, Z{}, ma, mb, m0, n0, sp.k0, n);
                 } else if (q.amn == MN_ROWS) {
-                    if (q.bmn == MN_ROWS) stream(R{}, R{}, ma, mb, m0, n0, n);
-                    else stream(R{}, Z{}, ma, mb, m0, n0, n);
+                    if (q.bmn == MN_ROWS) stream(R{}, R{}, ma, mb, m0, n0, sp.k0, n);
+                    else stream(R{}, Z{}, ma, mb, m0, n0, sp.k0, n);
                 } else {
-                    if (q.bmn == MN_ROWS) stream(Z{}, R{}, ma, mb, m0, n0, n);
-                    else stream(Z{}, Z{}, ma, mb, m0, n0, n);
+                    if (q.bmn == MN_ROWS) stream(Z{}, R{}, ma, mb, m0, n0, sp.k0, n);
+                    else stream(Z{}, Z{}, ma, mb, m0, n0, sp.k0, n);
                 }
             }
         }
@@ -386,7 +400,7 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
                 if (tl.p < 0) break;
                 const GemmProb& q = a.p[tl.p];
                 const bool amn = q.amn != 0, bmn = q.bmn != 0;
-                const int kbs = q.kb, buf = i & 1;
+                const int kbs = gm_span(q, tl.m).kb, buf = i & 1;
                 const uint32_t idesc = idesc_bf16(256, BN, amn) | ((bmn ? 1u : 0u) << 16);
                 // 16 k-elements on.  K-major: 32 bytes in the swizzled row; MN-major: 16 rows of 128 bytes
                 const uint32_t da = (amn ? 2048u : 32u) >> 4, db = (bmn ? 2048u : 32u) >> 4;
@@ -445,7 +459,8 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
             const GemmProb& pr = a.p[tl.p];
             const int kind = pr.kind, N = pr.N, out = pr.out, buf = i & 1;
             const int tn = kind == GM_GATE ? BN / 2 : BN, w = tn / 2;          // the tile's and this warp's columns
-            const int row0 = (tl.m * S::PM + pm) * 256 + half * 128 + quarter * 32, n0 = (tl.n * S::PN + pn) * tn + side * w;
+            const GmSpan sp = gm_span(pr, tl.m);
+            const int row0 = (sp.m * S::PM + pm) * 256 + half * 128 + quarter * 32, n0 = (tl.n * S::PN + pn) * tn + side * w;
             const uint32_t acc = tmem + (uint32_t)(buf * BN + side * w) + ((uint32_t)(quarter * 32) << 16);
             const int end = row0 < pr.M ? min(w, N - n0) : 0;                  // columns there are; may be negative
             Pq8 pp[4], qq[4];
@@ -557,7 +572,7 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
                     stage_full();
                     if (lane == 0) {
                         if (kind == GM_ADD) gm_store_add(&maps.o[out], stage, n0 + c, row0);
-                        else gm_store(&maps.o[out], stage, n0 + c, row0);
+                        else gm_store(&maps.o[out], stage, n0 + c, row0 + sp.row);
                         gm_store_commit();
                     }
                 }
@@ -577,6 +592,20 @@ __global__ void __launch_bounds__(GM_NT, 1) k_mlp_gemm(const __grid_constant__ G
 
 // ---- host ----
 
+// With few rows of tiles the sums over F (y, dx) leave most SMs without work: up to JOIN_T tokens they may be cut into
+// parts, in fp32 and added up by k_mlp_join, at most 8 and JOIN_ROWS rows of them (8 KB of workspace a channel).  us of a
+// forward and a backward, cut where the plan says so / never: C = 2048, F = 5632: - and 48 / 57 at T = 32, 34 / 36 and
+// 55 / 60 at 256, 46 / 48 and 66 / 71 at 512; C = 4096, F = 11008: 83 / 89 and 145 / 157 at 200.
+constexpr int JOIN_T = 1024, JOIN_ROWS = 2048;
+constexpr int JOIN_CLOCKS = 9500, JOIN_BYTES = 4000;   // its launch and what a cut costs besides; bytes a clock
+int join_rows(int64_t T) { return (int)((T + 31) / 32 * 32); }   // rows of a part: whole boxes
+int join_parts(int64_t T) {
+    if (T > JOIN_T) return 1;
+    int s = 8;
+    while (s * join_rows(T) > JOIN_ROWS) s /= 2;
+    return s;
+}
+
 using GmTall = GmShape<2, 1, 256>;
 using GmPair = GmShape<1, 1, 256>;
 using GmWide = GmShape<1, 2, 128>;
@@ -590,7 +619,8 @@ int64_t gm_tiles(GemmArgs& a, int clusters) {
     for (int p = 0; p < a.nprob; ++p) {
         GemmProb& q = a.p[p];
         const int bm = 256 * S::PM, tn = (q.kind == GM_GATE ? S::BN / 2 : S::BN) * S::PN;
-        q.tm = (q.M + bm - 1) / bm;
+        q.part_tm = (q.M + bm - 1) / bm;
+        q.tm = q.part_tm * q.split;
         q.tn = (q.N + tn - 1) / tn;
         q.group = S::GROUP;
         q.first = a.tiles;
@@ -653,16 +683,16 @@ cudaError_t gm_fit(int* n) {
     if (keep && (*n = fit[dev].load(std::memory_order_relaxed)) > 0) return cudaSuccess;
     cudaLaunchAttribute at[2];
     const cudaLaunchConfig_t cfg = gm_config<S>(at, device_sms() / S::CTAS);
+    if ((e = smem_optin((const void*)k_mlp_gemm<S>, S::SMEM)) != cudaSuccess) return e;
     e = cudaOccupancyMaxActiveClusters(n, k_mlp_gemm<S>, &cfg);
     if (e == cudaSuccess && keep) fit[dev].store(*n, std::memory_order_relaxed);
     return e;
 }
 template <class S>
 cudaError_t gm_try(GemmArgs& a, int shape, GmPlan* best) {
-    cudaError_t e = smem_optin((const void*)k_mlp_gemm<S>, S::SMEM);
-    if (e != cudaSuccess) return e;
     int n = 0;
-    if ((e = gm_fit<S>(&n)) != cudaSuccess) return e;
+    const cudaError_t e = gm_fit<S>(&n);
+    if (e != cudaSuccess) return e;
     if (n < 1) return cudaSuccess;
     const int64_t clocks = gm_tiles<S>(a, n);
     if (best->clocks < 0 || clocks < best->clocks) {
@@ -688,7 +718,9 @@ cudaError_t gm_launch(const GemmMaps& maps, GemmArgs& a, int clusters, bool foll
     cudaLaunchConfig_t cfg = gm_config<S>(at, a.tiles < clusters ? a.tiles : clusters);
     cfg.stream = st;
     cfg.numAttrs = follow || pdl_on() ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_mlp_gemm<S>, maps, a);
+    cudaError_t e = smem_optin((const void*)k_mlp_gemm<S>, S::SMEM);
+    if (e != cudaSuccess) return e;
+    e = cudaLaunchKernelEx(&cfg, k_mlp_gemm<S>, maps, a);
     note_launch();
     return e == cudaSuccess ? cudaGetLastError() : e;
 }
@@ -713,7 +745,82 @@ GemmProb gm_prob(int M, int N, int K, int kind, int set, int out) {
     p.kind = kind;
     p.set = set;
     p.out = out;
+    p.split = 1;
     return p;
+}
+// The sum of `pairs` operand pairs in `parts` parts, stored in fp32 one below the other (k_mlp_join adds them)
+void gm_split(GemmProb* p, int pairs, int parts) {
+    p->split = parts;
+    while (pairs << p->shift < parts) ++p->shift;
+    p->kb = (p->kb1 + (1 << p->shift) - 1) >> p->shift;
+    p->part_rows = join_rows(p->M);
+    p->kind = GM_F32;
+}
+
+// out[t][c] = the sum of the parts' values, in order: 8 channels a thread
+constexpr int JOIN_NT = 256;
+template <int PARTS>
+__global__ void __launch_bounds__(JOIN_NT) k_mlp_join(int64_t n, int64_t stride, const float* part, uint16_t* out) {
+    pdl_entry();
+    const int64_t i = ((int64_t)blockIdx.x * JOIN_NT + threadIdx.x) * 8;
+    if (i >= n) return;
+    float4 v[PARTS][2];
+#pragma unroll
+    for (int s = 0; s < PARTS; ++s)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) v[s][e] = *reinterpret_cast<const float4*>(part + s * stride + i + 4 * e);
+    float o[8] = {};
+#pragma unroll
+    for (int s = 0; s < PARTS; ++s)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            o[4 * e] += v[s][e].x;
+            o[4 * e + 1] += v[s][e].y;
+            o[4 * e + 2] += v[s][e].z;
+            o[4 * e + 3] += v[s][e].w;
+        }
+    *reinterpret_cast<uint4*>(out + i) = pack8(o);
+}
+template <int PARTS>
+cudaError_t join_run(int T, int C, const float* part, uint16_t* out, cudaStream_t st) {
+    const int64_t n = (int64_t)T * C;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((n / 8 + JOIN_NT - 1) / JOIN_NT));
+    cfg.blockDim = dim3(JOIN_NT);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, k_mlp_join<PARTS>, n, (int64_t)join_rows(T) * C, part, out);
+    note_launch();
+    return e == cudaSuccess ? cudaGetLastError() : e;
+}
+cudaError_t launch_join(int parts, int T, int C, const float* part, uint16_t* out, cudaStream_t st) {
+    if (parts == 2) return join_run<2>(T, C, part, out, st);
+    if (parts == 4) return join_run<4>(T, C, part, out, st);
+    return join_run<8>(T, C, part, out, st);
+}
+
+// The launch that takes the fewest clocks of those with the sum whole or in 2, 4, .. parts (build(parts): its
+// problems), with k_mlp_join's own
+template <class Build>
+cudaError_t gm_plan_parts(int T, int C, int pairs, int kb1, const Build& build, GemmArgs* a, GmPlan* pl, int* parts) {
+    const int most = join_parts(T);
+    for (int s = 1; s <= most; s *= 2) {
+        if (s > 1 && (s < pairs || s / pairs > kb1)) continue;
+        GemmArgs b = build(s);
+        GmPlan p;
+        const cudaError_t e = gm_plan(b, &p);
+        if (e != cudaSuccess) return e;
+        if (s > 1) p.clocks += JOIN_CLOCKS + (int64_t)s * join_rows(T) * C * 8 / JOIN_BYTES;
+        if (s > 1 && p.clocks >= pl->clocks) continue;
+        *a = b;
+        *pl = p;
+        *parts = s;
+    }
+    return cudaSuccess;
 }
 GemmArgs gm_args(int nprob, int* err) {
     GemmArgs a = {};
@@ -747,8 +854,14 @@ bool map_out(CUtensorMap* m, const void* p, int rows, int cols, bool f32, int by
                bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+// the output of a sum that may be in parts
+bool map_joined(CUtensorMap* m, const uint16_t* out, const float* part, int T, int C, int parts) {
+    return parts > 1 ? map_out(m, part, parts * join_rows(T), C, true, 128) : map_out(m, out, T, C, false, 128);
+}
 
 }  // namespace
+
+size_t mlp_part_bytes(int64_t T, int C) { return join_parts(T) > 1 ? (size_t)join_parts(T) * join_rows(T) * C * 4 : 0; }
 
 size_t mlp_pq_bytes(int64_t T, int F) { return (size_t)((T + 31) / 32) * (F / 8) * PQ_BLOCK; }
 
@@ -769,17 +882,23 @@ cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, con
     return gm_run(m, a, pl, 1, 2, 1, false, st);
 }
 
-cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, int* err,
+cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, float* part, int* err,
                             cudaStream_t st) {
-    GemmArgs a = gm_args(1, err);
-    a.p[0] = gm_prob(T, C, F, GM_BF16, 0, 0);
+    GemmArgs a;
     GmPlan pl;
-    const cudaError_t e = gm_plan(a, &pl);
+    int parts;
+    const cudaError_t e = gm_plan_parts(T, C, 1, (F + GM_BK - 1) / GM_BK, [&](int s) {
+        GemmArgs b = gm_args(1, err);
+        b.p[0] = gm_prob(T, C, F, GM_BF16, 0, 0);
+        if (s > 1) gm_split(&b.p[0], 1, s);
+        return b;
+    }, &a, &pl, &parts);
     if (e != cudaSuccess) return e;
     GemmMaps m = {};
-    if (!map_k(&m.a[0], h, T, F, pl.a_rows()) || !map_k(&m.b[0], Wd, C, F, pl.b_rows()) || !map_out(&m.o[0], y, T, C, false, 128))
+    if (!map_k(&m.a[0], h, T, F, pl.a_rows()) || !map_k(&m.b[0], Wd, C, F, pl.b_rows()) || !map_joined(&m.o[0], y, part, T, C, parts))
         return cudaErrorInvalidValue;
-    return gm_run(m, a, pl, 1, 1, 1, true, st);
+    const cudaError_t r = gm_run(m, a, pl, 1, 1, 1, true, st);
+    return r == cudaSuccess && parts > 1 ? launch_join(parts, T, C, part, y, st) : r;
 }
 
 cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uint16_t* Wd, const uint16_t* h, const void* pq,
@@ -806,29 +925,37 @@ cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uin
 
 cudaError_t launch_mlp_dx_dw(int T, int C, int F, const uint16_t* x, const uint16_t* dg, const uint16_t* du,
                              const uint16_t* Wg, const uint16_t* Wu, uint16_t* dx, void* dWg, void* dWu, int f32,
-                             int accumulate, int* err, cudaStream_t st) {
-    GemmArgs a = gm_args(3, err);
+                             int accumulate, float* part, int* err, cudaStream_t st) {
     const int kind = !f32 ? GM_BF16 : accumulate ? GM_ADD : GM_F32;
-    GemmProb d = gm_prob(T, C, F, GM_BF16, 0, 0);
-    d.kb = 2 * d.kb1;
-    const GemmProb w = gm_prob(F, C, T, kind, 2, 1), v = gm_prob(F, C, T, kind, 3, 2);
-    const int id = d.kb >= w.kb ? 0 : 2, ig = d.kb >= w.kb ? 1 : 0;   // the longer tiles first
-    a.p[id] = d;
-    a.p[ig] = w;
-    a.p[ig + 1] = v;
+    GemmArgs a;
     GmPlan pl;
-    const cudaError_t e = gm_plan(a, &pl);
+    int parts;
+    auto order = [](const GemmProb& dx, const GemmProb& dw) { return dx.kb >= dw.kb; };   // the longer tiles first
+    const cudaError_t e = gm_plan_parts(T, C, 2, (F + GM_BK - 1) / GM_BK, [&](int s) {
+        GemmArgs b = gm_args(3, err);
+        GemmProb d = gm_prob(T, C, F, GM_BF16, 0, 0);
+        d.kb = 2 * d.kb1;
+        if (s > 1) gm_split(&d, 2, s);
+        const GemmProb w = gm_prob(F, C, T, kind, 2, 1);
+        const int first = order(d, w) ? 1 : 0;
+        b.p[first ? 0 : 2] = d;
+        b.p[first] = w;
+        b.p[first + 1] = gm_prob(F, C, T, kind, 3, 2);
+        return b;
+    }, &a, &pl, &parts);
     if (e != cudaSuccess) return e;
+    const int id = a.p[0].set == 0 ? 0 : 2, ig = id == 0 ? 1 : 0;
     GemmMaps m = {};
     if (!map_k(&m.a[0], dg, T, F, pl.a_rows()) || !map_k(&m.a[1], du, T, F, pl.a_rows()) || !map_mn(&m.b[0], Wg, F, C, pl.b_rows(), &a.p[id].bmn) ||
         !map_mn(&m.b[1], Wu, F, C, pl.b_rows(), &a.p[id].bmn) || !map_mn(&m.a[2], dg, T, F, pl.a_rows(), &a.p[ig].amn) ||
         !map_mn(&m.a[3], du, T, F, pl.a_rows(), &a.p[ig + 1].amn) || !map_mn(&m.b[2], x, T, C, pl.b_rows(), &a.p[ig].bmn) ||
-        !map_out(&m.o[0], dx, T, C, false, 128) || !map_out(&m.o[1], dWg, F, C, f32 != 0, 128) ||
+        !map_joined(&m.o[0], dx, part, T, C, parts) || !map_out(&m.o[1], dWg, F, C, f32 != 0, 128) ||
         !map_out(&m.o[2], dWu, F, C, f32 != 0, 128))
         return cudaErrorInvalidValue;
     m.b[3] = m.b[2];
     a.p[ig + 1].bmn = a.p[ig].bmn;
-    return gm_run(m, a, pl, 4, 4, 3, true, st);
+    const cudaError_t r = gm_run(m, a, pl, 4, 4, 3, true, st);
+    return r == cudaSuccess && parts > 1 ? launch_join(parts, T, C, part, dx, st) : r;
 }
 
 }  // namespace xhc

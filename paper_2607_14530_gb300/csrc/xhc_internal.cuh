@@ -740,7 +740,9 @@ size_t mlp_pq_bytes(int64_t T, int F);
 // h = q u; pq: p = u act'(g), then q = act(g) (null: only h)
 cudaError_t launch_mlp_gate(int T, int C, int F, int act, const uint16_t* x, const uint16_t* Wg, const uint16_t* Wu,
                             uint16_t* h, void* pq, int* err, cudaStream_t st);
-cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, int* err,
+// part: mlp_part_bytes of scratch, for sums over F in parts
+size_t mlp_part_bytes(int64_t T, int C);
+cudaError_t launch_mlp_down(int T, int C, int F, const uint16_t* h, const uint16_t* Wd, uint16_t* y, float* part, int* err,
                             cudaStream_t st);
 // the forward's two products for few tokens; the second is launched right after the first
 bool mlp_small(int64_t T, int C, int F);   // whether these are few
@@ -754,6 +756,6 @@ cudaError_t launch_mlp_dh_dwd(int T, int C, int F, const uint16_t* dy, const uin
 // dx = dg W_gate + du W_up, dW_gate = dg^T x, dW_up = du^T x
 cudaError_t launch_mlp_dx_dw(int T, int C, int F, const uint16_t* x, const uint16_t* dg, const uint16_t* du,
                              const uint16_t* Wg, const uint16_t* Wu, uint16_t* dx, void* dWg, void* dWu, int f32,
-                             int accumulate, int* err, cudaStream_t st);
+                             int accumulate, float* part, int* err, cudaStream_t st);
 
 }  // namespace xhc

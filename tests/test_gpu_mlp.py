@@ -201,3 +201,26 @@ def test_device_error_word():
     ws[:4].view(torch.int32).fill_(13)
     torch.cuda.synchronize()
     assert op.device_error(ws) == 13 and op.device_error(ws, clear=True) == 13 and op.device_error(ws) == 0
+
+
+@pytest.mark.parametrize("T,C,F", [(1, 136, 8200), (33, 264, 8200), (256, 520, 8192), (257, 264, 12296), (513, 136, 8200),
+                                   (1024, 264, 8200), (1025, 264, 8200)])
+def test_sums_in_parts(T, C, F):
+    """Few tiles and long sums over F (cut into parts, up to 1024 tokens): y and dx against the 64-bit forms, the same
+    bits again and from a captured graph, and nothing written beyond the workspace."""
+    x, P, dy = inputs(T, C, F, seed=T)
+    x, op = x.cuda(), Mlp(C, F)
+    got = run(op, x, P, dy)
+    R.assert_mlp(got, R.mlp(x, P, "silu", dy))
+    room = Guarded(torch.zeros(op.workspace_bytes(T), dtype=torch.uint8))
+    saved, grads = op.alloc_saved(T), {n: torch.empty_like(v) for n, v in P.items()}
+    y, dx = op.forward(P, x, room.t, saved=saved), op.backward(P, x, dy, grads, saved, room.t)
+    graph = torch.cuda.CUDAGraph()
+    y2, dx2 = torch.empty_like(x), torch.empty_like(x)
+    with torch.cuda.graph(graph):
+        op.forward(P, x, room.t, saved=saved, y=y2)
+        op.backward(P, x, dy, grads, saved, room.t, dx=dx2)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert room.intact() and all(torch.equal(a, b) for a, b in ((y, got["y"]), (dx, got["dx"]), (y2, got["y"]), (dx2, got["dx"])))
+    assert all(torch.equal(v, got[n]) for n, v in grads.items())
