@@ -560,15 +560,34 @@ class Group:
 # ---- operators around the connection op ----
 
 
-def _arg(t, name, dtype, shape=None):
-    """The pointer of an operand: contiguous, of that type and shape, on the current CUDA device."""
+def _place(t, name):
+    """The device of a call's first operand, which has to be the current one."""
+    dev = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if dev < 0:
+        raise XhcError(f"{name} must be a CUDA tensor")
+    if dev != torch._C._cuda_getDevice():
+        raise XhcError(f"{name} is on cuda:{dev}, which is not the current device")
+    return dev
+
+
+def _arg(t, name, dtype, dev, shape=None):
+    """The pointer of an operand: contiguous, of that type and shape, on the call's device.  (Checks that pass
+    come first: a small call takes as long as they do.)"""
+    try:
+        if t.dtype is dtype and t.get_device() == dev and t.is_contiguous() and (shape is None or t.shape == shape):
+            return t.data_ptr()
+    except AttributeError:
+        pass
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.get_device() < 0 or not t.is_contiguous():
         raise XhcError(f"{name} must be a contiguous {str(dtype)[6:]} CUDA tensor")
-    if shape is not None and t.shape != shape:
-        raise XhcError(f"{name} must be of shape {list(shape)}, got {list(t.shape)}")
-    if t.get_device() != torch._C._cuda_getDevice():
+    if t.get_device() != dev:
         raise XhcError(f"{name} is on cuda:{t.get_device()}, which is not the current device")
-    return t.data_ptr()
+    raise XhcError(f"{name} must be of shape {list(shape)}, got {list(t.shape)}")
+
+
+def _stream_on(stream, dev):
+    """_stream of a call whose device is known to be the current one."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
 
 
 def _alloc(stream, *args, **kw):
@@ -580,9 +599,9 @@ def _alloc(stream, *args, **kw):
         return torch.empty(*args, **kw)
 
 
-def _buffer(t, name, nbytes):
+def _buffer(t, name, nbytes, dev):
     """The pointer of a `saved` or `workspace` buffer (uint8, at least nbytes)."""
-    p = _arg(t, name, torch.uint8)
+    p = _arg(t, name, torch.uint8, dev)
     if t.numel() < nbytes:
         raise XhcError(f"{name} has {t.numel()} bytes, {nbytes} are needed")
     return p
@@ -640,40 +659,45 @@ class Mlp:
     def shapes(self) -> dict:
         return {"W_gate": (self.F, self.C), "W_up": (self.F, self.C), "W_down": (self.C, self.F)}
 
-    def _weights(self, d: dict, what: str, dtype) -> _MlpWeights:
+    def _weights(self, d: dict, what: str, dtype, dev) -> _MlpWeights:
         C, F = self.C, self.F
-        return _MlpWeights(_arg(d.get("W_gate"), what + "W_gate", dtype, (F, C)), _arg(d.get("W_up"), what + "W_up", dtype, (F, C)),
-                           _arg(d.get("W_down"), what + "W_down", dtype, (C, F)))
+        return _MlpWeights(_arg(d.get("W_gate"), what + "W_gate", dtype, dev, (F, C)),
+                           _arg(d.get("W_up"), what + "W_up", dtype, dev, (F, C)),
+                           _arg(d.get("W_down"), what + "W_down", dtype, dev, (C, F)))
 
     def forward(self, P: dict, x, ws, saved=None, y=None, stream=None):
         """y [T, C] of x [T, C].  ``saved``: what the backward needs is kept there (None: no backward)."""
         bf, T = torch.bfloat16, x.shape[0]
-        px = _arg(x, "x", bf, (T, self.C))
+        dev = _place(x, "x")
+        px = _arg(x, "x", bf, dev, (T, self.C))
         if y is None:
             y = _alloc(stream, T, self.C, dtype=bf, device=x.device)
         nsaved, nws = self._bytes(T)
-        W = self._weights(P, "", bf)
-        _check(lib().xhc_mlp_fwd(self._c, T, W, px, _arg(y, "y", bf, (T, self.C)),
-                                 None if saved is None else _buffer(saved, "saved", nsaved), _buffer(ws, "ws", nws),
-                                 _stream(stream)), "xhc_mlp_fwd")
+        W = self._weights(P, "", bf, dev)
+        _check(lib().xhc_mlp_fwd(self._c, T, W, px, _arg(y, "y", bf, dev, (T, self.C)),
+                                 None if saved is None else _buffer(saved, "saved", nsaved, dev), _buffer(ws, "ws", nws, dev),
+                                 _stream_on(stream, dev)), "xhc_mlp_fwd")
         return y
 
     def backward(self, P: dict, x, dy, grads: dict, saved, ws, dx=None, accumulate=False, stream=None):
         """dx [T, C]; the weight gradients go into ``grads``."""
         bf, T = torch.bfloat16, x.shape[0]
-        px = _arg(x, "x", bf, (T, self.C))
+        dev = _place(x, "x")
+        px = _arg(x, "x", bf, dev, (T, self.C))
         if dx is None:
             dx = _alloc(stream, T, self.C, dtype=bf, device=x.device)
         nsaved, nws = self._bytes(T)
-        W = self._weights(P, "", bf)
+        W = self._weights(P, "", bf, dev)
         gt = getattr(grads.get("W_gate"), "dtype", None)
         if gt not in (torch.float32, bf):
             raise XhcError("weight gradients must be fp32 or bf16 CUDA tensors")
         if accumulate and gt is bf:
             raise XhcError("bf16 weight gradients are written, not accumulated: use fp32 ones")
-        _check(lib().xhc_mlp_bwd(self._c, T, W, px, _arg(dy, "dy", bf, (T, self.C)), _arg(dx, "dx", bf, (T, self.C)),
-                                 self._weights(grads, "gradient of ", gt), 1 if gt is bf else 0, 1 if accumulate else 0,
-                                 _buffer(saved, "saved", nsaved), _buffer(ws, "ws", nws), _stream(stream)), "xhc_mlp_bwd")
+        _check(lib().xhc_mlp_bwd(self._c, T, W, px, _arg(dy, "dy", bf, dev, (T, self.C)),
+                                 _arg(dx, "dx", bf, dev, (T, self.C)),
+                                 self._weights(grads, "gradient of ", gt, dev), 1 if gt is bf else 0, 1 if accumulate else 0,
+                                 _buffer(saved, "saved", nsaved, dev), _buffer(ws, "ws", nws, dev), _stream_on(stream, dev)),
+               "xhc_mlp_bwd")
         return dx
 
 
@@ -714,34 +738,36 @@ class SumNorm:
         """Scratch of the backward."""
         return torch.empty(self.workspace_bytes(T), dtype=torch.uint8, device=device)
 
-    def _state(self, t, name, T):
-        return _arg(t, name, torch.bfloat16, (T, self.C) if self.N == 1 and t.dim() == 2 else (T, self.N, self.C))
+    def _state(self, t, name, T, dev):
+        return _arg(t, name, torch.bfloat16, dev, (T, self.C) if self.N == 1 and t.dim() == 2 else (T, self.N, self.C))
 
     def forward(self, w, X, y=None, saved=None, stream=None):
         bf, T = torch.bfloat16, X.shape[0]
-        pX = self._state(X, "X", T)
+        dev = _place(X, "X")
+        pX = self._state(X, "X", T, dev)
         if y is None:
             y = _alloc(stream, T, self.C, dtype=bf, device=X.device)
-        _check(lib().xhc_sum_norm_fwd(self.N, self.C, self.eps, T, pX, _arg(w, "w", torch.float32, (self.C,)),
-                                      _arg(y, "y", bf, (T, self.C)),
-                                      None if saved is None else _buffer(saved, "saved", self._bytes(T)[0]), _stream(stream)),
+        _check(lib().xhc_sum_norm_fwd(self.N, self.C, self.eps, T, pX, _arg(w, "w", torch.float32, dev, (self.C,)),
+                                      _arg(y, "y", bf, dev, (T, self.C)),
+                                      None if saved is None else _buffer(saved, "saved", self._bytes(T)[0], dev),
+                                      _stream_on(stream, dev)),
                "xhc_sum_norm_fwd")
         return y
 
     def backward(self, w, X, dy, dw, saved, ws, dX=None, accumulate=False, stream=None):
         """dX, shaped like X (with N > 1 X is not read and may be None); dw [C] fp32 is written, or
         added to with ``accumulate``."""
-        T = dy.shape[0]
+        T, dev = dy.shape[0], _place(dy, "dy")
         if X is None and self.N == 1:
             raise XhcError("X is needed with N = 1")
-        pX = None if X is None else self._state(X, "X", T)
+        pX = None if X is None else self._state(X, "X", T, dev)
         if dX is None:
             dX = _alloc(stream, (T, self.N, self.C) if X is None else X.shape, dtype=torch.bfloat16, device=dy.device)
         nsaved, nws = self._bytes(T)
-        _check(lib().xhc_sum_norm_bwd(self.N, self.C, T, pX, _arg(w, "w", torch.float32, (self.C,)),
-                                      _arg(dy, "dy", torch.bfloat16, (T, self.C)), self._state(dX, "dX", T),
-                                      _arg(dw, "dw", torch.float32, (self.C,)), 1 if accumulate else 0,
-                                      _buffer(saved, "saved", nsaved), _buffer(ws, "ws", nws), _stream(stream)),
+        _check(lib().xhc_sum_norm_bwd(self.N, self.C, T, pX, _arg(w, "w", torch.float32, dev, (self.C,)),
+                                      _arg(dy, "dy", torch.bfloat16, dev, (T, self.C)), self._state(dX, "dX", T, dev),
+                                      _arg(dw, "dw", torch.float32, dev, (self.C,)), 1 if accumulate else 0,
+                                      _buffer(saved, "saved", nsaved, dev), _buffer(ws, "ws", nws, dev), _stream_on(stream, dev)),
                "xhc_sum_norm_bwd")
         return dX
 
@@ -785,17 +811,17 @@ def clip_grads(grads, max_norm: float, scale: float = 1.0, eps: float = 1e-6, ou
             raise XhcError("every gradient needs an output, and no other")
         out = [o for o in out if o is not None]
     grads = [g for g in grads if g is not None]
-    n, device = len(grads), torch.cuda.current_device()
+    n, device, Tensor = len(grads), torch.cuda.current_device(), torch.Tensor
 
     def checked(ts, what):
         """The pointers, sizes and types of a list of tensors."""
-        if [t.get_device() for t in ts].count(device) != len(ts) or False in [t.is_contiguous() for t in ts]:
+        if list(map(Tensor.get_device, ts)).count(device) != len(ts) or False in map(Tensor.is_contiguous, ts):
             q = [t.get_device() == device and t.is_contiguous() for t in ts].index(False)
             raise XhcError(f"{what} {q} must be a contiguous CUDA tensor on the current device")
         types = [t.dtype for t in ts]
         if not _CLIP_TYPES.issuperset(types):
             raise XhcError(f"every {what} must be an fp32 or bf16 tensor")
-        return [t.data_ptr() for t in ts], [t.numel() for t in ts], types
+        return list(map(Tensor.data_ptr, ts)), list(map(Tensor.numel, ts)), types
 
     ptrs, numel, types = checked(grads, "gradient")
     to = ptrs
@@ -814,6 +840,7 @@ def clip_grads(grads, max_norm: float, scale: float = 1.0, eps: float = 1e-6, ou
     a, c, d = array("q", ptrs), array("q", numel), array("i", [1 if t is torch.bfloat16 else 0 for t in types])
     b = None if out is None else array("q", to)
     _check(lib().xhc_clip_grads(n, a.buffer_info()[0], None if b is None else b.buffer_info()[0], c.buffer_info()[0],
-                                d.buffer_info()[0], scale, max_norm, eps, _arg(norm, "norm", torch.float32, (1,)),
-                                _buffer(ws, "ws", _clip_workspace_bytes()), _stream(stream)), "xhc_clip_grads")
+                                d.buffer_info()[0], scale, max_norm, eps, _arg(norm, "norm", torch.float32, device, (1,)),
+                                _buffer(ws, "ws", _clip_workspace_bytes(), device), _stream_on(stream, device)),
+           "xhc_clip_grads")
     return norm
